@@ -261,6 +261,43 @@ hs_status hs_draft_static(hs_ctx* ctx, const hs_draft_args* args, const hs_seq_s
 hs_status hs_draft_group(hs_ctx* ctx, const hs_group_draft_args* args, const hs_seq_state* seq, hs_step* step,
                          hs_stream stream);
 
+/* Sliding-window attention with sinks, per layer: window is a HOST array of n_layers entries (copied); in a layer with
+ * window[l] >= 1 a row at position p sees, of what it sees otherwise, the positions t > p - window[l] and the first
+ * `sinks` ones, t < sinks; 0 leaves the layer as it is.  NULL: no layer has a window.  hs_verify (with every flag) and
+ * hs_prefill follow it from the next call on; what a HIP graph has recorded keeps the windows of its recording.  A row's
+ * result does not depend on what other rows its sequence has, nor on how a text is cut into chunks, as without windows.
+ * Only pages that hold a position some row of the call sees are looked up and read: where all layers have windows, a page
+ * whose positions lie behind the window of every row to come and beyond the sinks may be given to another sequence (its
+ * entry in block_table is then not used any more; the entries of the sinks' pages and of the pages from there on are). */
+enum { HS_WINDOW_MAX = 1 << 30 };
+hs_status hs_set_window(hs_ctx* ctx, const int32_t* window, int32_t sinks);
+
+/* Attention of one layer with a sliding window and sinks on its own, for queries that the caller has: what hs_verify
+ * (chunk = 0) and hs_prefill (chunk > 0) run in a layer with a window.
+ *   chunk = 0: the rows are draft-tree nodes; row_off, row2seq, pos and anc_mask of `step` are read, with the meaning that
+ *     hs_draft gives them (pos = L_b + depth; at most 64 nodes per sequence; a single node is one-token decoding).  A cached
+ *     key's position is its slot, a node's is its pos.
+ *   chunk >= 1: the rows are consecutive tokens, row i of sequence b at position (and slot) seq_len[b] - 1 + i, which sees no
+ *     position beyond its own; of `step` only row_off is read.  chunk = the most rows of a sequence that the launch is shaped
+ *     for (more are computed, too, only slower).  Not with the plain-kernel flags.
+ * out[row][h] = sum_t softmax_t(q[row][h] . k[t][h / G] / sqrt(head_dim)) v[t][h / G] over the visible t, G = n_q_heads /
+ * n_kv_heads; zeros for a row that sees nothing (an empty anc_mask, pages missing from the block table: a position whose
+ * table entry is no page of the cache, or lies beyond the table, is not seen).  K and V of the rows themselves are read from the cache: hs_verify
+ * and hs_prefill write them, a caller of this function has.  What a row does not see has no influence on it, infinities and
+ * NaNs included.  Rows from row_off[batch] on are left as they are.  With HS_FLAG_FP32_ACTIVATIONS q and out are floats (and
+ * the cache is).  The partial results lie in the workspace: calls that share it are ordered by the caller, as those of
+ * hs_verify are; the range of V that hs_verify states applies to chunk = 0. */
+typedef struct hs_window_args {
+    int32_t layer;
+    int32_t window;     /* 1..HS_WINDOW_MAX */
+    int32_t sinks;      /* 0..HS_WINDOW_MAX */
+    int32_t chunk;
+    const void* q;      /* DEVICE bf16 [rows][n_q_heads][head_dim], rotated, 16-byte aligned */
+    void* out;          /* DEVICE bf16, same shape and alignment; may be q */
+} hs_window_args;
+hs_status hs_attention_window(hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step,
+                              const hs_window_args* args, hs_stream stream);
+
 /* One target-model forward pass over all M rows (Sec. 2.2).  Writes every row's K/V into the cache at slot
  * L_b + node index, attends over positions [0, L_b) plus the node's ancestors-or-self, and writes
  * (Numerical range: the attention runs split over key partitions whose partial outputs -- each a convex combination
@@ -298,6 +335,48 @@ hs_status hs_prefill(hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* 
  * sampling keeps per-row sums in the workspace during the call; calls with step arrays and logits of their own may
  * overlap on different streams all the same (a call sums again what another one has overwritten). */
 hs_status hs_accept(hs_ctx* ctx, const hs_accept_args* args, const hs_seq_state* seq, hs_step* step, hs_stream stream);
+
+/* Probabilities of rows of logits: out[i][t] = exp((logits[i][t] - max) / temperature) / sum, t < vocab, in 32 bits and
+ * rounded once to out_type.  An excluded token (-inf) gets 0, a row of nothing else zeros; a NaN or +inf makes its row NaN.
+ * Rows from `rows` (or from *live_rows, if that is given and smaller) on, and what lies behind the vocabulary in a row, are
+ * left as they are.  Strides are in elements, >= vocab; rows need their element's alignment only (16-byte aligned rows are
+ * faster).  The logits may be those of hs_verify or of any other model over the same vocabulary.  Scratch lies in the workspace:
+ * calls that share it are ordered by the caller. */
+enum { HS_F32 = 0, HS_BF16 = 1 };   /* element types of hs_probs and hs_accept_probs */
+typedef struct hs_probs_args {
+    const void* logits;         /* DEVICE [rows][logits_stride] */
+    void* out;                  /* DEVICE [rows][out_stride]; may be logits, with the same type and stride */
+    int64_t logits_stride, out_stride;
+    int32_t logits_type, out_type;
+    int32_t rows;               /* HOST: >= 0 */
+    float temperature;          /* > 0 */
+    const int32_t* live_rows;   /* DEVICE, optional: how many of the rows there are (e.g. row_off + batch) */
+} hs_probs_args;
+hs_status hs_probs(hs_ctx* ctx, const hs_probs_args* args, hs_stream stream);
+
+/* Acceptance against given probabilities with given random numbers: in place of hs_accept where drafts were drawn from a
+ * distribution, the target's probabilities have been filtered, or the random numbers are the caller's.  Row i of p is the
+ * target's distribution behind node i, row i of q the one from which the node's children were drawn, independently of each
+ * other.  At a node, w_0 = p, Z_0 = 1; its children are tried in node order; child number k with token t is accepted if
+ *     u_accept[child's row] * Z_k * q(t) < w_k(t)
+ * and otherwise leaves w_{k+1} = max(w_k - Z_k q, 0), Z_{k+1} = the sum of w_{k+1}.  With q = NULL drafts have no distribution
+ * (they come from a history): 1 stands for q(t), and w_{k+1} is w_k without t.  Where no child is accepted (or there is none)
+ * the last token is the first one at which the running sum of w in token order exceeds u_sample[b] * (the sum of w); if w is
+ * empty, w = p; if that is empty, too, it is token vocab - 1.  The emitted tokens are distributed as the target's own if the
+ * numbers are uniform on [0, 1) and independent.  All of this is computed in 64 bits.  A probability that is negative, not
+ * finite or a NaN counts as 0; so does that of a drafted id outside the vocabulary.  Rows of p need not add up to exactly 1.
+ * Writes accept_len, n_out, out_tok and path_row as hs_accept does (hs_kv_commit follows); argmax is not touched.  Sums lie in
+ * the workspace: calls that share it are ordered by the caller. */
+typedef struct hs_accept_probs_args {
+    const void* p;              /* DEVICE [M][p_stride] */
+    const void* q;              /* DEVICE [M][q_stride], or NULL */
+    int64_t p_stride, q_stride; /* elements between rows, >= vocab (q_stride is not read without q) */
+    int32_t type;               /* HS_F32 or HS_BF16, of p and q */
+    const float* u_accept;      /* DEVICE [M]: entry i decides on node i (roots' entries are not read) */
+    const float* u_sample;      /* DEVICE [batch] */
+} hs_accept_probs_args;
+hs_status hs_accept_probs(hs_ctx* ctx, const hs_accept_probs_args* args, const hs_seq_state* seq, hs_step* step,
+                          hs_stream stream);
 
 /* Moves accepted nodes' K/V to consecutive slots L_b+1.. (a no-op for a chain), then seq_len += n_out,
  * budget_left -= n_out, tail/tokens/k_state/counters updated. */

@@ -23,6 +23,8 @@ HS_K_FIXED, HS_K_MATCHLEN, HS_K_AIMD = 0, 1, 2
 HS_ACCEPT_GREEDY, HS_ACCEPT_REJECTION = 0, 1
 HS_FLAG_REFERENCE_KERNELS, HS_FLAG_FP32_ACTIVATIONS, HS_FLAG_WORKSPACE_LOGITS = 1, 2, 4
 HS_GATE_WORDS, HS_GATE_TABLE = 32, 8
+HS_F32, HS_BF16 = 0, 1
+HS_WINDOW_MAX = 1 << 30
 
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -114,13 +116,29 @@ class hs_prefill_args(C.Structure):
     _fields_ = [("chunk", C.c_int32), ("rows_hint", C.c_int32), ("kv_done", C.c_void_p)]
 
 
+class hs_window_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("layer", "window", "sinks", "chunk")] + [("q", C.c_void_p), ("out", C.c_void_p)]
+
+
+class hs_probs_args(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("out", C.c_void_p), ("logits_stride", C.c_int64), ("out_stride", C.c_int64),
+                ("logits_type", C.c_int32), ("out_type", C.c_int32), ("rows", C.c_int32), ("temperature", C.c_float),
+                ("live_rows", C.c_void_p)]
+
+
+class hs_accept_probs_args(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("q", C.c_void_p), ("p_stride", C.c_int64), ("q_stride", C.c_int64), ("type", C.c_int32),
+                ("u_accept", C.c_void_p), ("u_sample", C.c_void_p)]
+
+
 HS_PREFILL_CHUNK_MAX = 1024
 
 
 EXPORTS = ("hs_create", "hs_destroy", "hs_last_error", "hs_set_flags", "hs_workspace_bytes", "hs_bind_workspace",
            "hs_draft", "hs_draft_group", "hs_verify", "hs_accept", "hs_kv_commit", "hs_poll_error", "hs_debug_buffer",
            "hs_set_profile", "hs_get_profile", "hs_debug_gemm", "hs_gate_table_build", "hs_prefill", "hs_plan_allocation",
-           "hs_debug_capture", "hs_debug_capture_bytes", "hs_debug_philox", "hs_draft_static", "hs_accept_commit", "hs_debug_rowmax_groups")
+           "hs_debug_capture", "hs_debug_capture_bytes", "hs_debug_philox", "hs_draft_static", "hs_accept_commit", "hs_debug_rowmax_groups",
+           "hs_set_window", "hs_attention_window", "hs_probs", "hs_accept_probs")
 
 _lib = None
 
@@ -159,6 +177,11 @@ def lib():
         L.hs_debug_rowmax_groups.argtypes = [C.c_int32]
         L.hs_accept_commit.argtypes = [vp, C.POINTER(hs_accept_args), C.POINTER(hs_kv_cache), C.POINTER(hs_seq_state),
                                        C.POINTER(hs_step), C.POINTER(hs_policy), vp]
+        L.hs_set_window.argtypes = [vp, C.POINTER(C.c_int32), C.c_int32]
+        L.hs_attention_window.argtypes = [vp, C.POINTER(hs_kv_cache), C.POINTER(hs_seq_state), C.POINTER(hs_step),
+                                          C.POINTER(hs_window_args), vp]
+        L.hs_probs.argtypes = [vp, C.POINTER(hs_probs_args), vp]
+        L.hs_accept_probs.argtypes = [vp, C.POINTER(hs_accept_probs_args), C.POINTER(hs_seq_state), C.POINTER(hs_step), vp]
         L.hs_poll_error.argtypes = [vp, vp, C.POINTER(C.c_uint32)]
         L.hs_debug_buffer.argtypes = [vp, C.c_int32, C.POINTER(vp), C.POINTER(C.c_size_t)]
         L.hs_debug_capture_bytes.argtypes = [vp]
@@ -246,6 +269,24 @@ def hs_accept_commit(ctx, args: hs_accept_args, cache: hs_kv_cache, seq: hs_seq_
                      policy: hs_policy, stream=None):
     _check(ctx, lib().hs_accept_commit(ctx, C.byref(args), C.byref(cache), C.byref(seq), C.byref(step),
                                        C.byref(policy), stream))
+
+
+def hs_set_window(ctx, window, sinks: int = 0):
+    """window: one entry per layer (0 = the layer has none), or None to switch windows off."""
+    arr = None if window is None else (C.c_int32 * len(window))(*[int(x) for x in window])
+    _check(ctx, lib().hs_set_window(ctx, arr, int(sinks)))
+
+
+def hs_attention_window(ctx, cache: hs_kv_cache, seq: hs_seq_state, step: hs_step, args: hs_window_args, stream=None):
+    _check(ctx, lib().hs_attention_window(ctx, C.byref(cache), C.byref(seq), C.byref(step), C.byref(args), stream))
+
+
+def hs_probs(ctx, args: hs_probs_args, stream=None):
+    _check(ctx, lib().hs_probs(ctx, C.byref(args), stream))
+
+
+def hs_accept_probs(ctx, args: hs_accept_probs_args, seq: hs_seq_state, step: hs_step, stream=None):
+    _check(ctx, lib().hs_accept_probs(ctx, C.byref(args), C.byref(seq), C.byref(step), stream))
 
 
 def hs_poll_error(ctx, stream=None) -> int:

@@ -58,6 +58,7 @@ void layout_workspace(hs_ctx* ctx) {
     w.att_list = take(2 * hs_attention_max_units(ctx) * 32);
     w.reject_walk = take((size_t)l.max_batch * 16);
     w.reject_stats = take(M * (size_t)hs_reject_slices(d.vocab) * sizeof(hs_reject_stat));
+    w.probs_sums = take((size_t)HS_PROBS_ROUNDS * l.max_batch * hs_probs_slices(d.vocab) * sizeof(double));
     w.total = off;
 }
 
@@ -111,6 +112,12 @@ bool policy_ok(const hs_ctx* ctx, const hs_policy* p) {
 }
 
 bool cache_ok(const hs_kv_cache* c) { return c && c->k && c->v && c->n_blocks >= 1; }
+
+bool type_ok(int type) { return type == HS_F32 || type == HS_BF16; }
+// rows over the vocabulary: their stride, and their elements' own alignment
+bool rows_ok(const hs_ctx* ctx, const void* p, long long stride, int type) {
+    return stride >= ctx->desc.vocab && ((uintptr_t)p & (type == HS_F32 ? 3u : 1u)) == 0;
+}
 
 }  // namespace
 
@@ -236,6 +243,21 @@ hs_status hs_set_flags(hs_ctx* ctx, uint32_t flags) {
     return HS_OK;
 }
 
+hs_status hs_set_window(hs_ctx* ctx, const int32_t* window, int32_t sinks) {
+    if (!ctx) return HS_ERR_INVALID_ARG;
+    if (!window) {
+        ctx->window.clear();
+        ctx->sinks = 0;
+        return HS_OK;
+    }
+    if (sinks < 0 || sinks > HS_WINDOW_MAX) return fail(ctx, HS_ERR_INVALID_ARG, "hs_set_window: sinks");
+    for (int l = 0; l < ctx->desc.n_layers; l++)
+        if (window[l] < 0 || window[l] > HS_WINDOW_MAX) return fail(ctx, HS_ERR_INVALID_ARG, "hs_set_window: window");
+    ctx->window.assign(window, window + ctx->desc.n_layers);
+    ctx->sinks = sinks;
+    return HS_OK;
+}
+
 size_t hs_workspace_bytes(const hs_ctx* ctx) { return ctx ? ctx->lay.total : 0; }
 
 hs_status hs_bind_workspace(hs_ctx* ctx, void* dev_ptr, size_t bytes) {
@@ -356,11 +378,15 @@ hs_status hs_verify(hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* s
         pr.begin(3);
         hs_launch_rope_kv(ctx, l, cache, seq, step, qkv, q, pend, expected, st);
         pr.end();
+        const int window = hs_window_of(ctx, l);
+        const bool windowed = window > 0 && !hs_plain_kernels(ctx);
         pr.begin(0, l % 4 == 0);
-        hs_launch_attention(ctx, l, cache, seq, step, q, attn, st);
+        if (windowed) hs_launch_window_attention(ctx, l, cache, seq, step, q, attn, window, ctx->sinks, st);
+        else hs_launch_attention(ctx, l, cache, seq, step, q, attn, st, window, ctx->sinks);
         pr.end();
         pr.begin(3);
-        hs_launch_attention_merge(ctx, seq, step, attn, expected, st);
+        if (windowed) hs_launch_window_merge(ctx, cache, seq, step, attn, window, ctx->sinks, st);
+        else hs_launch_attention_merge(ctx, seq, step, attn, expected, st);
         pr.end();
         pr.begin(1);
         hs_launch_gemm(ctx, HS_EPI_ADD_F32, attn, ctx->wo[l], nullptr, x, m_dev, m_max, d.d_model, qh, hint, st, &pend, fold);
@@ -449,7 +475,9 @@ hs_status hs_prefill(hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* 
         hs_launch_rope_kv(ctx, l, cache, &pf, step, qkv, q, pend, expected, st);
         pend = {};
         if (l + 1 == d.n_layers) break;   // the last layer's K/V are written: nothing downstream is needed
-        hs_launch_attention_prefill(ctx, l, cache, &pf, len_plus1, step, q, attn, args->chunk, st);
+        if (const int window = hs_window_of(ctx, l); window > 0)
+            hs_launch_window_chunk(ctx, l, cache, &pf, len_plus1, step, q, attn, args->chunk, window, ctx->sinks, st);
+        else hs_launch_attention_prefill(ctx, l, cache, &pf, len_plus1, step, q, attn, args->chunk, st);
         hs_launch_gemm(ctx, HS_EPI_ADD_F32, attn, ctx->wo[l], nullptr, x, m_dev, m_max, d.d_model, qh, hint, st, &pend, fold);
         hs_launch_rmsnorm(ctx, x, ctx->norm2[l], xn, m_dev, pend, expected, st);
         hs_launch_gemm(ctx, HS_EPI_SWIGLU_BF16, xn, ctx->wgate[l], ctx->wup[l], act, m_dev, m_max, d.d_ffn, d.d_model, hint, st);
@@ -519,6 +547,77 @@ hs_status hs_accept_commit(hs_ctx* ctx, const hs_accept_args* args, const hs_kv_
     if (!ctx) return HS_ERR_INVALID_ARG;
     if (!args || !policy) return fail(ctx, HS_ERR_INVALID_ARG, "hs_accept_commit: arguments");
     return accept_commit(ctx, "hs_accept_commit", args, cache, seq, step, policy, stream);
+}
+
+hs_status hs_accept_probs(hs_ctx* ctx, const hs_accept_probs_args* args, const hs_seq_state* seq, hs_step* step,
+                          hs_stream stream) {
+    if (!ctx) return HS_ERR_INVALID_ARG;
+    if (!ctx->ws) return fail(ctx, HS_ERR_CAPACITY, "no workspace bound");
+    if (!args || !args->p || !args->u_accept || !args->u_sample)
+        return fail(ctx, HS_ERR_INVALID_ARG, "hs_accept_probs: null probabilities or random numbers");
+    if (!type_ok(args->type)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_accept_probs: type");
+    if (!rows_ok(ctx, args->p, args->p_stride, args->type) || (args->q && !rows_ok(ctx, args->q, args->q_stride, args->type)))
+        return fail(ctx, HS_ERR_INVALID_ARG, "hs_accept_probs: stride below the vocabulary, or misaligned rows");
+    if (!seq_ok(ctx, seq)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_accept_probs: sequence state");
+    if (!step_ok(step)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_accept_probs: step arrays");
+    (void)hipGetLastError();
+    hs_launch_accept_probs(ctx, args, seq, step, (hipStream_t)stream);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail_hip(ctx, "hs_accept_probs", e);
+    return HS_OK;
+}
+
+hs_status hs_probs(hs_ctx* ctx, const hs_probs_args* args, hs_stream stream) {
+    if (!ctx) return HS_ERR_INVALID_ARG;
+    if (!ctx->ws) return fail(ctx, HS_ERR_CAPACITY, "no workspace bound");
+    if (!args || !args->logits || !args->out) return fail(ctx, HS_ERR_INVALID_ARG, "hs_probs: null logits or output");
+    if (!type_ok(args->logits_type) || !type_ok(args->out_type)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_probs: type");
+    if (!(args->temperature > 0.f)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_probs: temperature must be positive");
+    if (args->rows < 0) return fail(ctx, HS_ERR_INVALID_ARG, "hs_probs: rows");
+    if (!rows_ok(ctx, args->logits, args->logits_stride, args->logits_type) || !rows_ok(ctx, args->out, args->out_stride, args->out_type))
+        return fail(ctx, HS_ERR_INVALID_ARG, "hs_probs: stride below the vocabulary, or misaligned rows");
+    if (args->out == args->logits && (args->out_type != args->logits_type || args->out_stride != args->logits_stride))
+        return fail(ctx, HS_ERR_INVALID_ARG, "hs_probs: in place with another type or stride");
+    if (args->rows == 0) return HS_OK;
+    (void)hipGetLastError();
+    hs_launch_probs(ctx, args, (hipStream_t)stream);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail_hip(ctx, "hs_probs", e);
+    return HS_OK;
+}
+
+hs_status hs_attention_window(hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step,
+                              const hs_window_args* args, hs_stream stream) {
+    if (!ctx) return HS_ERR_INVALID_ARG;
+    if (!ctx->ws) return fail(ctx, HS_ERR_CAPACITY, "no workspace bound");
+    if (!cache_ok(cache)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_window: cache");
+    if (!seq_ok(ctx, seq)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_window: sequence state");
+    if (!args || !args->q || !args->out) return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_window: null queries or output");
+    if ((((uintptr_t)args->q | (uintptr_t)args->out) & 15u) != 0)
+        return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_window: queries and output must be 16-byte aligned");
+    if (args->layer < 0 || args->layer >= ctx->desc.n_layers) return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_window: layer");
+    if (args->window < 1 || args->window > HS_WINDOW_MAX || args->sinks < 0 || args->sinks > HS_WINDOW_MAX)
+        return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_window: window or sinks");
+    if (args->chunk < 0) return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_window: chunk");
+    if (!step || !step->row_off) return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_window: step arrays");
+    const hipStream_t st = (hipStream_t)stream;
+    if (args->chunk > 0) {
+        if (args->chunk > ctx->lim.max_rows) return fail(ctx, HS_ERR_CAPACITY, "hs_attention_window: chunk beyond max_rows");
+        if (hs_plain_kernels(ctx)) return fail(ctx, HS_ERR_UNSUPPORTED, "hs_attention_window: no plain-kernel mode for chunks");
+        (void)hipGetLastError();
+        hs_launch_window_chunk(ctx, args->layer, cache, seq, seq->seq_len, step, args->q, args->out, args->chunk, args->window,
+                               args->sinks, st);
+    } else {
+        if (!step->pos || !step->anc_mask || !step->row2seq)
+            return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_window: step arrays");
+        (void)hipGetLastError();
+        if (hs_plain_kernels(ctx)) {
+            hs_launch_attention(ctx, args->layer, cache, seq, step, args->q, args->out, st, args->window, args->sinks);
+        } else {
+            hs_launch_window_attention(ctx, args->layer, cache, seq, step, args->q, args->out, args->window, args->sinks, st);
+            hs_launch_window_merge(ctx, cache, seq, step, args->out, args->window, args->sinks, st);
+        }
+    }
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail_hip(ctx, "hs_attention_window", e);
+    return HS_OK;
 }
 
 hs_status hs_poll_error(hs_ctx* ctx, hs_stream stream, uint32_t* error_bits) {

@@ -830,7 +830,8 @@ __global__ __launch_bounds__(64) void attn_verify_plain(
     const T* __restrict__ q, const T* __restrict__ kc, const T* __restrict__ vc, size_t layer_off,
     const int32_t* __restrict__ seq_len, const int32_t* __restrict__ block_table, int max_blocks, int n_blocks,
     const int32_t* __restrict__ row_off, const int32_t* __restrict__ row2seq, const uint64_t* __restrict__ anc_mask,
-    int batch, int hq, int hkv, int hd, float scale, T* __restrict__ out) {
+    const int32_t* __restrict__ pos, int window, int sinks, int batch, int hq, int hkv, int hd, float scale,
+    T* __restrict__ out) {
     constexpr bool PRECISE = sizeof(ACC) == 8;
     int row = blockIdx.x, head = blockIdx.y, lane = threadIdx.x;
     if (row >= row_off[batch]) return;
@@ -844,6 +845,10 @@ __global__ __launch_bounds__(64) void attn_verify_plain(
     ACC m = -INFINITY, l = 0, o0 = 0, o1 = 0;
     for (int kp = 0; kp < total; kp++) {
         bool vis = kp < L || ((anc >> (kp - L)) & 1ull);
+        if (vis && window > 0) {
+            const int at = kp < L ? kp : pos[row_off[b] + kp - L];
+            vis = at > pos[row] - window || at < sinks;
+        }
         if (!vis) continue;
         if ((kp >> 4) >= max_blocks) break;
         int page = block_table[(size_t)b * max_blocks + (kp >> 4)];
@@ -878,8 +883,8 @@ __global__ __launch_bounds__(64) void attn_verify_plain(
         m = mn;
     }
     T* op = out + ((size_t)row * hq + head) * hd;
-    if (lane < hd) plain_st(op + lane, (double)(o0 / l));
-    if (lane + 64 < hd) plain_st(op + lane + 64, (double)(o1 / l));
+    if (lane < hd) plain_st(op + lane, l == 0 ? 0.0 : (double)(o0 / l));      // (a row that sees nothing)
+    if (lane + 64 < hd) plain_st(op + lane + 64, l == 0 ? 0.0 : (double)(o1 / l));
 }
 
 template <int HD>
@@ -922,7 +927,7 @@ void launch_mfma(const hs_ctx* ctx, int layer, size_t layer_off, const hs_kv_cac
 }  // namespace
 
 void hs_launch_attention(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const hs_seq_state* seq,
-                         const hs_step* step, const void* q_any, void* out, hipStream_t st) {
+                         const hs_step* step, const void* q_any, void* out, hipStream_t st, int window, int sinks) {
     const hs_model_desc& d = ctx->desc;
     size_t layer_off = (size_t)layer * cache->n_blocks * d.n_kv_heads * 16 * d.head_dim;
     if (hs_plain_kernels(ctx)) {
@@ -932,13 +937,13 @@ void hs_launch_attention(const hs_ctx* ctx, int layer, const hs_kv_cache* cache,
             hipLaunchKernelGGL((attn_verify_plain<float, double>), grid, dim3(64), 0, st, (const float*)q_any,
                                (const float*)cache->k, (const float*)cache->v, layer_off, seq->seq_len,
                                seq->block_table, ctx->lim.max_blocks_per_seq, cache->n_blocks, step->row_off,
-                               step->row2seq, step->anc_mask, seq->batch, d.n_q_heads, d.n_kv_heads, d.head_dim,
+                               step->row2seq, step->anc_mask, step->pos, window, sinks, seq->batch, d.n_q_heads, d.n_kv_heads, d.head_dim,
                                scale, (float*)out);
         else
             hipLaunchKernelGGL((attn_verify_plain<bf16_t, float>), grid, dim3(64), 0, st, (const bf16_t*)q_any,
                                (const bf16_t*)cache->k, (const bf16_t*)cache->v, layer_off, seq->seq_len,
                                seq->block_table, ctx->lim.max_blocks_per_seq, cache->n_blocks, step->row_off,
-                               step->row2seq, step->anc_mask, seq->batch, d.n_q_heads, d.n_kv_heads, d.head_dim,
+                               step->row2seq, step->anc_mask, step->pos, window, sinks, seq->batch, d.n_q_heads, d.n_kv_heads, d.head_dim,
                                scale, (bf16_t*)out);
         return;
     }

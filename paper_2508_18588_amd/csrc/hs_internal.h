@@ -25,8 +25,13 @@ constexpr int HS_REJECT_SLICE = 4096;
 struct alignas(16) hs_reject_stat { float m; uint32_t check; double s; };
 static inline int hs_reject_slices(int vocab) { return (vocab + HS_REJECT_SLICE - 1) / HS_REJECT_SLICE; }
 
+// Verification against probabilities: the vocabulary is summed in slices of this many tokens, for each sequence in up to
+// HS_PROBS_ROUNDS launches.
+constexpr int HS_PROBS_SLICE = 4096, HS_PROBS_ROUNDS = 2;
+static inline int hs_probs_slices(int vocab) { return (vocab + HS_PROBS_SLICE - 1) / HS_PROBS_SLICE; }
+
 struct hs_workspace_layout {
-    size_t x, xn, qkv, q, attn, act, part_o, part_ml, logits, logits_bytes, rowmax, draft_best, gemm_part, gemm_part_bytes, err, pf_len, row_info, att_work, att_list, reject_stats, reject_walk, total;
+    size_t x, xn, qkv, q, attn, act, part_o, part_ml, logits, logits_bytes, rowmax, draft_best, gemm_part, gemm_part_bytes, err, pf_len, row_info, att_work, att_list, reject_stats, reject_walk, probs_sums, total;
 };
 
 struct hs_ctx {
@@ -37,6 +42,8 @@ struct hs_ctx {
     std::vector<const bf16_t*> wqkv, wo, wgate, wup, wdown;
     std::vector<const float*> norm1, norm2;
     uint32_t flags = 0;
+    std::vector<int32_t> window;   // hs_set_window: per layer, 0 = none; empty: no layer has one
+    int32_t sinks = 0;
     char* capture = nullptr;  // hs_debug_capture: snapshots of the last layer's projection inputs
     char* ws = nullptr;
     size_t ws_bytes = 0;
@@ -77,6 +84,7 @@ static inline bool hs_plain_kernels(const hs_ctx* ctx) {
 }
 int hs_gemm_chunks(int n, int k);
 int hs_gemm_chunks(int n, int k, bool narrow);   // with groups of 64 (narrow) or 128 weight rows
+static inline int hs_window_of(const hs_ctx* ctx, int layer) { return ctx->window.empty() ? 0 : ctx->window[layer]; }
 // Must the logits exist as an [rows][vocab] array?  Yes if the caller asks for them (a destination in the step, or
 // HS_FLAG_WORKSPACE_LOGITS), with the plain kernels, and when the LM head splits K (a small vocabulary).  Otherwise the
 // LM head reduces every row to its argmax in its epilogue and hs_accept finishes the reduction.
@@ -179,8 +187,16 @@ void hs_launch_rmsnorm(const hs_ctx* ctx, float* x, const float* w, void* out, c
 void hs_launch_rope_kv(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const hs_seq_state* seq,
                        const hs_step* step, const float* qkv, void* q, hs_pending pending, int expected,
                        hipStream_t st);
+// (window > 0: that window and sinks, with the plain kernels only)
 void hs_launch_attention(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const hs_seq_state* seq,
-                         const hs_step* step, const void* q, void* out, hipStream_t st);
+                         const hs_step* step, const void* q, void* out, hipStream_t st, int window = 0, int sinks = 0);
+// Attention with a sliding window and sinks (hs_window.hip): a draft's rows, whose partial results the merge joins, and a chunk's.
+void hs_launch_window_attention(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step,
+                                const void* q, void* out, int window, int sinks, hipStream_t st);
+void hs_launch_window_merge(const hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step, void* out,
+                            int window, int sinks, hipStream_t st);
+void hs_launch_window_chunk(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const hs_seq_state* seq, const int32_t* len_plus1,
+                            const hs_step* step, const void* q, void* out, int chunk, int window, int sinks, hipStream_t st);
 // Chunked prefill: row arrays of one call (rows of sequence b = its next tokens from the token log) and the causal
 // attention over [0, kv_done + i] for token i of the chunk.  len_plus1[b] = cached positions + 1.
 void hs_launch_prefill_rows(const hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, int32_t* kv_done, int chunk, hs_step* step,
@@ -216,3 +232,7 @@ void hs_launch_draft_group(const hs_ctx* ctx, const hs_group_draft_args* args, c
 void hs_launch_accept_commit(const hs_ctx* ctx, const hs_accept_args* args, const hs_kv_cache* cache,
                              const hs_seq_state* seq, const hs_step* step, const float* logits,
                              const unsigned long long* keys, int n_keys, const hs_policy* policy, hipStream_t st);
+// Softmax of logits, and acceptance against given probabilities (hs_probs.hip).
+void hs_launch_probs(const hs_ctx* ctx, const hs_probs_args* args, hipStream_t st);
+void hs_launch_accept_probs(const hs_ctx* ctx, const hs_accept_probs_args* args, const hs_seq_state* seq, const hs_step* step,
+                            hipStream_t st);

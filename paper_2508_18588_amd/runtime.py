@@ -13,7 +13,8 @@ import torch
 from . import (HS_FLAG_WORKSPACE_LOGITS, hs_accept_commit, HS_FLAG_FP32_ACTIVATIONS, hs_debug_capture, hs_debug_capture_bytes, HS_ACCEPT_GREEDY, HS_GATE_TABLE, HS_GATE_WORDS, HS_K_FIXED, hs_gate_table_build, hs_accept, hs_accept_args, hs_bind_workspace, hs_create, hs_debug_buffer, hs_debug_gemm,
                hs_destroy, hs_draft, hs_draft_args, hs_draft_group, hs_group_draft_args, hs_get_profile, hs_kv_cache, hs_kv_commit, hs_limits,
                hs_model_desc, hs_policy, hs_poll_error, hs_prefill, hs_prefill_args, hs_seq_state, hs_set_flags, hs_set_profile, hs_step,
-               hs_verify, hs_weights, hs_workspace_bytes)
+               hs_verify, hs_weights, hs_workspace_bytes, HS_BF16, HS_F32, hs_accept_probs, hs_accept_probs_args,
+               hs_attention_window, hs_probs, hs_probs_args, hs_set_window, hs_window_args)
 
 
 @dataclass
@@ -43,6 +44,14 @@ def _dev(a, dtype=None):
         a = a.view(np.int64)
     t = torch.from_numpy(a).cuda()
     return t if dtype is None else t.to(dtype)
+
+
+def _type(t: torch.Tensor) -> int:
+    """HS_F32 or HS_BF16 of a tensor of rows over the vocabulary."""
+    kinds = {torch.float32: HS_F32, torch.bfloat16: HS_BF16}
+    if t.dtype not in kinds or t.dim() != 2 or t.stride(1) != 1:
+        raise ValueError(f"rows of float32 or bfloat16 expected, got {t.dtype} of shape {tuple(t.shape)}, strides {t.stride()}")
+    return kinds[t.dtype]
 
 
 class Engine:
@@ -305,6 +314,47 @@ class Engine:
     @staticmethod
     def gate_table(ms, rows, k_bar: float, b_max: int):
         return hs_gate_table_build(ms, rows, k_bar, b_max)
+
+    # ---------------------------------------------------------------- windows, probabilities
+
+    def set_window(self, window, sinks: int = 0):
+        """Sliding-window attention with sinks in verify() and the prefills: one window for all layers, a list with one per
+        layer (0 = none), or None to switch it off."""
+        if isinstance(window, int):
+            window = [window] * self.n_layers
+        if window is not None and len(window) != self.n_layers:
+            raise ValueError(f"{len(window)} windows for {self.n_layers} layers")
+        hs_set_window(self.ctx, window, sinks)
+
+    def attention_window(self, layer: int, q, out, window: int, sinks: int = 0, chunk: int = 0):
+        """One layer's attention with a window and sinks for the queries q [rows, n_q_heads * head_dim] of the rows laid out in
+        the step arrays (chunk = 0), or of up to `chunk` consecutive tokens per sequence (row_off alone)."""
+        if q.dtype != out.dtype or q.dtype != (torch.float32 if self.precise else torch.bfloat16):
+            raise ValueError(f"queries and output of {q.dtype}, {out.dtype}")
+        if not (q.is_contiguous() and out.is_contiguous()):
+            raise ValueError("queries and output must be contiguous")
+        hs_attention_window(self.ctx, self.c_cache, self.c_seq, self.c_step,
+                            hs_window_args(layer, window, sinks, chunk, q.data_ptr(), out.data_ptr()), self.stream())
+
+    def probs(self, logits, out, temperature: float = 1.0, live: bool = False):
+        """out[i] = softmax(logits[i] / temperature) over the vocabulary, float32 or bfloat16 each; live: only the rows that
+        the step arrays hold."""
+        if min(logits.shape[1], out.shape[1]) < self.shape.vocab or out.shape[0] < logits.shape[0]:
+            raise ValueError(f"logits {tuple(logits.shape)}, output {tuple(out.shape)} for a vocabulary of {self.shape.vocab}")
+        args = hs_probs_args(logits.data_ptr(), out.data_ptr(), logits.stride(0), out.stride(0), _type(logits), _type(out),
+                             logits.shape[0], temperature, self.st["row_off"].data_ptr() + 4 * self.batch if live else None)
+        hs_probs(self.ctx, args, self.stream())
+
+    def accept_probs(self, p, q, u_accept, u_sample):
+        """Acceptance of the step's drafts against the target's probabilities p [rows, vocab] and the drafts' distributions q
+        (None: they have none), with u_accept [rows] and u_sample [batch] as random numbers; commit() follows."""
+        if q is not None and _type(q) != _type(p):
+            raise ValueError(f"probabilities of {p.dtype} and {q.dtype}")
+        if u_accept.dtype != torch.float32 or u_sample.dtype != torch.float32 or not (u_accept.is_contiguous() and u_sample.is_contiguous()):
+            raise ValueError("random numbers must be contiguous float32")
+        args = hs_accept_probs_args(p.data_ptr(), None if q is None else q.data_ptr(), p.stride(0), 0 if q is None else q.stride(0),
+                                    _type(p), u_accept.data_ptr(), u_sample.data_ptr())
+        hs_accept_probs(self.ctx, args, self.c_seq, self.c_step, self.stream())
 
     def poll_error(self) -> int:
         return hs_poll_error(self.ctx, self.stream())
