@@ -9,6 +9,26 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A 32-key sub-tile (two pages) in LDS: K as 32 rows of HD elements, then V^T as two pages of HD rows of 16 tokens, both
+// without padding, so that a page's K or V^T block is one contiguous run that a load into LDS can fill.  16-byte chunks are
+// permuted instead: within a row of K, so that 16 consecutive rows read at the same chunk cover the 64 banks once; of 16 rows of
+// V^T first the first halves, then the second ones, so that an operand is two 8-byte pieces a constant distance apart.  (32 lanes
+// read the same half of their chunks, so two of them meet on each bank: the counters show LDS busy 50 % of the cycles, 20 of
+// them conflicts, where single 16-byte pieces had 23 % and none; a 14B step with trees 1388 -> 1391 us.)
+template <int HD>
+struct sub_tile {
+    static constexpr int PAGE = 32 * HD, V = 2 * PAGE, BYTES = 4 * PAGE;   // a page's K (or V^T) block, V^T's place, all
+    static __device__ __forceinline__ int k_at(int key, int chunk) {
+        return key * 2 * HD + ((chunk ^ (HD == 128 ? key & 15 : (key >> 1) & 7)) << 4);
+    }
+    // what 1 KB further on changes in the permutation
+    static constexpr int k_step(int i) { return (HD == 128 ? 4 * i & 15 : 4 * i & 7) << 4; }
+    static constexpr int V_HALF = 256;   // from a row's first to its second half
+    static __device__ __forceinline__ int v_at(int dim, int chunk) { return (dim >> 4) * 512 + chunk * V_HALF + (dim & 15) * 16; }
+    // where in a page's V^T block the 16 bytes that belong at 16 c of it in LDS come from
+    static __device__ __forceinline__ int v_from(int c) { return ((c >> 5) * 16 + (c & 15)) * 32 + ((c >> 4) & 1) * 16; }
+};
+
 // Query fragments (B operand of S^T) and ancestor mask of the lane's row; rows beyond R read as zero.
 template <int HD>
 __device__ inline void load_query_tile(const bf16_t* q, const uint64_t* anc_mask, int r0, int rt, int R, int G,

@@ -23,6 +23,9 @@
 
 namespace {
 
+// (a NaN stays one: the rounding alone would make an infinity of some)
+__device__ __forceinline__ bf16_t to_bf16(float v) { return __builtin_isnan(v) ? (bf16_t)0x7FC0 : f32_to_bf16(v); }
+
 struct win_args {
     const bf16_t *q, *kc, *vc;          // kc, vc: at the layer
     const int32_t *seq_len, *block_table, *row_off, *row2seq, *pos;
@@ -30,7 +33,7 @@ struct win_args {
     bf16_t* out;
     _Float16* part_o;
     float* part_ml;
-    int batch, max_blocks, n_blocks, hq, hkv, window, sinks, part_keys, max_parts;
+    int batch, max_blocks, n_blocks, hq, hkv, window, sinks, part_keys, max_parts, groups;
     float scale_log2;
 };
 
@@ -75,18 +78,110 @@ struct key_tile { bf16x8 k[HD / 16]; };
 template <int HD>
 struct value_tile { bf16x8 v[2][HD / 32]; };
 
-__device__ __forceinline__ bool has_nonfinite(const bf16x8& x) {
-    const u32x4 u = __builtin_bit_cast(u32x4, x);
+// Sets the elements that are infinities or NaNs to 0; true if there were any.
+__device__ __forceinline__ bool take_nonfinite(bf16x8& x) {
+    u32x4 u = __builtin_bit_cast(u32x4, x);
     bool any = false;
 #pragma unroll
-    for (int i = 0; i < 4; i++) any |= (u[i] & 0x7F80u) == 0x7F80u || (u[i] & 0x7F800000u) == 0x7F800000u;
+    for (int i = 0; i < 4; i++) {
+        const bool lo = (u[i] & 0x7F80u) == 0x7F80u, hi = (u[i] & 0x7F800000u) == 0x7F800000u;
+        any |= lo | hi;
+        u[i] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+    }
+    x = __builtin_bit_cast(bf16x8, u);
     return any;
+}
+
+// The pages of a tile's keys; -1: there is none, or no row sees a key of it.
+struct places { int p0, p1; };
+
+// What a row sees of a tile that not every row sees all of: bit e of the result, for key e of the lane's.
+template <int HD>
+__device__ __forceinline__ unsigned seen_keys(const win_args& a, const win_span& s, const row_tile<HD>& t, const places& here, int kb, int half) {
+    unsigned seen = 0;
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+        const int key = kb + 16 * (e >> 3) + 8 * half + (e & 7), node = key - s.L;
+        // (no branches: the shift's amount is taken modulo 64, and a node's bit counts between 0 and 63)
+        const bool old = (key < t.hi) & ((key >= t.lo) | (key < a.sinks));
+        const bool vis = (old | (((unsigned)node < 64u) & (bool)((t.anc >> (node & 63)) & 1ull))) & ((e < 8 ? here.p0 : here.p1) >= 0);
+        seen |= (unsigned)vis << e;
+    }
+    return seen;
+}
+__device__ __forceinline__ bool tile_masked(const win_args& a, const places& here, int kb, int all_lo, int all_hi) {
+    return (kb + 32 > all_hi) | ((kb < all_lo) & (kb + 32 > a.sinks)) | ((here.p0 | here.p1) < 0);
+}
+
+// Masks a tile's scores and moves the running maximum; returns what the sums so far are to be scaled by.
+template <int HD>
+__device__ __forceinline__ float take_scores(const win_args& a, const win_span& s, row_tile<HD>& t, f32x16& sc,
+                                             const places& here, bool masked, int kb, int half) {
+    constexpr int NDT = HD / 32;
+    if (masked) {
+        const unsigned seen = seen_keys<HD>(a, s, t, here, kb, half);
+#pragma unroll
+        for (int e = 0; e < 16; e++) sc[e] = (seen >> e) & 1u ? sc[e] : -INFINITY;
+    }
+    float tmax = sc[0];
+#pragma unroll
+    for (int e = 1; e < 16; e++) tmax = fmaxf(tmax, sc[e]);
+    {
+        // lanes l and l + 32 hold the two halves of a query row
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(tmax), __float_as_uint(tmax), false, false);
+        tmax = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.scale_log2;
+    }
+    const float m_new = fmaxf(t.m, tmax);
+    float alpha = 1.f;
+    if (__any(m_new != t.m)) {
+        alpha = fast_exp2(t.m - (m_new == -INFINITY ? 0.f : m_new));
+        t.m = m_new;
+#pragma unroll
+        for (int dt = 0; dt < NDT; dt++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) t.o[dt][e] *= alpha;
+    }
+    return alpha;
+}
+// Takes infinities and NaNs out of the values of a tile that not every row sees all of, since 0 times one of them is a NaN; true if there
+// were any (see add_odd).
+template <int HD>
+__device__ __forceinline__ bool mask_values(value_tile<HD>& v) {
+    bool odd = false;
+#pragma unroll
+    for (int pp = 0; pp < 2; pp++)
+#pragma unroll
+        for (int dt = 0; dt < HD / 32; dt++) odd |= take_nonfinite(v.v[pp][dt]);
+    return odd;
+}
+// Probabilities of a tile, as the second product's operand, and their sum.
+template <int HD>
+__device__ __forceinline__ void take_probabilities(const win_args& a, row_tile<HD>& t, const f32x16& sc, float alpha, bf16x8 (&pb)[2]) {
+    const float m_safe = t.m == -INFINITY ? 0.f : t.m;
+    float psum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+        // (probabilities are rounded to bf16, the matrix instruction's type: half a step, at most 2^-8, each; their sum is not)
+        const float p = fast_exp2(__builtin_fmaf(sc[e], a.scale_log2, -m_safe));
+        psum += p;
+        pb[e >> 3][e & 7] = (__bf16)p;
+    }
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(psum), __float_as_uint(psum), false, false);
+    t.l = __builtin_fmaf(t.l, alpha, __uint_as_float(sw[0]) + __uint_as_float(sw[1]));
+}
+template <int HD>
+__device__ __forceinline__ void take_values(row_tile<HD>& t, const value_tile<HD>& v, const bf16x8 (&pb)[2]) {
+#pragma unroll
+    for (int pp = 0; pp < 2; pp++)
+#pragma unroll
+        for (int dt = 0; dt < HD / 32; dt++)
+            t.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v[pp][dt], pb[pp], t.o[dt], 0, 0, 0);
 }
 
 // Walks keys k0, ... (32 at a time, k_end excluded) with one row tile.  all_lo, all_hi: every row sees the keys in [all_lo, all_hi) and
 // in [0, min(sinks, all_hi)).
 template <int HD>
-__device__ __forceinline__ void walk_keys(const win_args& a, const win_span& s, const int32_t* __restrict__ bt, int j, int k0, int k_end,
+__device__ __forceinline__ bool walk_keys(const win_args& a, const win_span& s, const int32_t* __restrict__ bt, int j, int k0, int k_end,
                                           int all_lo, int all_hi, row_tile<HD>& t, int lane) {
     constexpr int NKS = HD / 16, NDT = HD / 32;
     const int half = lane >> 5, l32 = lane & 31;
@@ -104,7 +199,6 @@ __device__ __forceinline__ void walk_keys(const win_args& a, const win_span& s, 
         if (at < a.max_blocks && p0 < k_end && (p0 < s.sink_end || p0 + 16 > s.first)) my_page = bt[at];
         if (my_page >= a.n_blocks) my_page = -1;
     };
-    struct places { int p0, p1; };
     auto find = [&](int kb) -> places {
         hold(kb);
         return {__builtin_amdgcn_readlane(my_page, (kb >> 4) & 63), __builtin_amdgcn_readlane(my_page, ((kb >> 4) & 63) + 1)};
@@ -124,7 +218,8 @@ __device__ __forceinline__ void walk_keys(const win_args& a, const win_span& s, 
         }
     };
 
-    if (k0 >= k_end) return;
+    bool odd = false;
+    if (k0 >= k_end) return odd;
     key_tile<HD> k;
     value_tile<HD> v;
     places cur = find(k0);
@@ -143,171 +238,394 @@ __device__ __forceinline__ void walk_keys(const win_args& a, const win_span& s, 
             cur = find(next);
             load_k(cur, k);
         }
-        const bool masked = kb + 32 > all_hi || !(kb >= all_lo || kb + 32 <= a.sinks) || here.p0 < 0 || here.p1 < 0;
-        unsigned seen = 0xFFFFu;        // bit e: the row sees key e of the lane's
-        if (masked) {
-            seen = 0;
-#pragma unroll
-            for (int e = 0; e < 16; e++) {
-                const int key = kb + 16 * (e >> 3) + 8 * half + (e & 7);
-                const bool old = key < t.hi && (key >= t.lo || key < a.sinks);
-                const bool node = key >= s.L && key - s.L < 64 && ((t.anc >> ((key - s.L) & 63)) & 1ull);
-                const bool vis = (old || node) && (e < 8 ? here.p0 : here.p1) >= 0;
-                sc[e] = vis ? sc[e] : -INFINITY;
-                seen |= (unsigned)vis << e;
-            }
-        }
-        float tmax = sc[0];
-#pragma unroll
-        for (int e = 1; e < 16; e++) tmax = fmaxf(tmax, sc[e]);
-        {
-            // lanes l and l + 32 hold the two halves of a query row
-            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(tmax), __float_as_uint(tmax), false, false);
-            tmax = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.scale_log2;
-        }
-        const float m_new = fmaxf(t.m, tmax);
-        float alpha = 1.f;
-        if (__any(m_new != t.m)) {
-            alpha = fast_exp2(t.m - (m_new == -INFINITY ? 0.f : m_new));
-            t.m = m_new;
-#pragma unroll
-            for (int dt = 0; dt < NDT; dt++)
-#pragma unroll
-                for (int e = 0; e < 16; e++) t.o[dt][e] *= alpha;
-        }
-        const float m_safe = t.m == -INFINITY ? 0.f : t.m;
-        float psum = 0.f;
         bf16x8 pb[2];
-#pragma unroll
-        for (int e = 0; e < 16; e++) {
-            // (probabilities are rounded to bf16, the matrix instruction's type: half a step, 2^-9, each; their sum is not)
-            const float p = fast_exp2(__builtin_fmaf(sc[e], a.scale_log2, -m_safe));
-            psum += p;
-            pb[e >> 3][e & 7] = (__bf16)p;
-        }
-        {
-            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(psum), __float_as_uint(psum), false, false);
-            t.l = __builtin_fmaf(t.l, alpha, __uint_as_float(sw[0]) + __uint_as_float(sw[1]));
-        }
-        bool odd = false;
-        if (masked) {
-#pragma unroll
-            for (int pp = 0; pp < 2; pp++)
-#pragma unroll
-                for (int dt = 0; dt < NDT; dt++) odd |= has_nonfinite(v.v[pp][dt]);
-        }
-        if (!__any(odd)) {
-#pragma unroll
-            for (int pp = 0; pp < 2; pp++)
-#pragma unroll
-                for (int dt = 0; dt < NDT; dt++)
-                    t.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v[pp][dt], pb[pp], t.o[dt], 0, 0, 0);
-        } else {
-            // An infinity or a NaN among the values of a tile that not every row sees all of: 0 times that is a NaN.  Token by
-            // token, and a row that does not see the token keeps what it had.
-#pragma unroll 1
-            for (int th = 0; th < 16; th++) {
-                const int th_half = th >> 3, th_at = th & 7;
-#pragma unroll
-                for (int pp = 0; pp < 2; pp++) {
-                    const unsigned bits = __shfl((int)seen, l32 + 32 * th_half);
-                    const bool sees = (bits >> (8 * pp + th_at)) & 1u;
-#pragma unroll
-                    for (int dt = 0; dt < NDT; dt++) {
-                        bf16x8 one;
-#pragma unroll
-                        for (int e = 0; e < 8; e++) one[e] = half == th_half && e == th_at ? v.v[pp][dt][e] : (__bf16)0.f;
-                        const f32x16 with = __builtin_amdgcn_mfma_f32_32x32x16_bf16(one, pb[pp], t.o[dt], 0, 0, 0);
-#pragma unroll
-                        for (int e = 0; e < 16; e++) t.o[dt][e] = sees ? with[e] : t.o[dt][e];
-                    }
-                }
-            }
-        }
-        if (!more) return;
+        const bool masked = tile_masked(a, here, kb, all_lo, all_hi);
+        const float alpha = take_scores<HD>(a, s, t, sc, here, masked, kb, half);
+        take_probabilities<HD>(a, t, sc, alpha, pb);
+        if (masked) odd |= mask_values<HD>(v);
+        take_values<HD>(t, v, pb);
+        if (!more) return __any(odd);
         load_v(cur, v);
         kb = next;
     }
 }
 
-// The rows of a draft (any number of nodes, a single token among them).  A workgroup takes four partitions of one (sequence, KV head)
-// with all row tiles: its wavefronts take (partition, row tile) pairs in turn, neighbours share a partition's keys.
+// Where the values of a tile that not every row sees all of held infinities or NaNs: the rows that do see them add them, element by
+// element, with the weights that they have in the end.  Keys k0, ... as in walk_keys, which has left them out.
 template <int HD>
-__global__ __launch_bounds__(256, 2) void window_rows(win_args a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
-    const int groups = (a.max_parts + 3) / 4;
-    const int g = blockIdx.x % groups, pair = blockIdx.x / groups;
-    const int j = pair % a.hkv, b = pair / a.hkv;
-    const int r0 = a.row_off[b], nn = a.row_off[b + 1] - r0;
-    const win_span s = make_span(a.seq_len[b], nn, a);
-    if (4 * g >= s.n_parts) return;
-    const int G = a.hq / a.hkv, R = nn * G, nrt = (R + 31) >> 5;
-    const int32_t* bt = a.block_table + (size_t)b * a.max_blocks;
-    const int items = min(4, s.n_parts - 4 * g) * nrt;
-    for (int it = wave; it < items; it += 4) {
-        const int c = 4 * g + it / nrt, rt = it % nrt;
-        row_tile<HD> t;
-        load_query_tile<HD>(a.q, a.anc_mask, r0, rt, R, G, a.hq, j, half, l32, t.qf, t.anc);
+__device__ __forceinline__ void add_odd(const win_args& a, const win_span& s, const int32_t* __restrict__ bt, int j, int k0, int k_end,
+                                     int all_lo, int all_hi, row_tile<HD>& t, int lane) {
+    const int half = lane >> 5, l32 = lane & 31;
+    auto page = [&](int pos) {
+        const int at = pos >> 4;
+        const int p = at < a.max_blocks && pos < k_end && (pos < s.sink_end || pos + 16 > s.first) ? bt[at] : -1;
+        return p < a.n_blocks ? p : -1;
+    };
+#pragma unroll 1
+    for (int kb = k0; kb < k_end; kb = s.skip(kb + 32)) {
+        const places here = {page(kb), page(kb + 16)};
+        if (!tile_masked(a, here, kb, all_lo, all_hi)) continue;
+        const bf16_t* kp = a.kc + ((size_t)max(l32 < 16 ? here.p0 : here.p1, 0) * a.hkv + j) * 16 * HD + page_order(l32 & 15) * HD + half * 8;
+        f32x16 sc;
 #pragma unroll
-        for (int dt = 0; dt < HD / 32; dt++)
+        for (int e = 0; e < 16; e++) sc[e] = 0.f;
 #pragma unroll
-            for (int e = 0; e < 16; e++) t.o[dt][e] = 0.f;
-        t.m = -INFINITY;
-        t.l = 0.f;
-        // the row's window; its depth is below nn, so that from all_lo on every row sees every cached key
-        const int all_lo = max(0, s.L + nn - a.window), rho = rt * 32 + l32;
-        const int pos = rho < R ? max(a.pos[r0 + rho / G], 0) : s.L;
-        t.lo = min(max(pos + 1 - a.window, s.first), all_lo);
-        t.hi = s.L;
-        if (a.window < HS_MAX_NODES) {
-            // ancestors that lie behind the window
-            uint64_t left = t.anc;
-            for (uint64_t todo = t.anc; todo; todo &= todo - 1) {
-                const int i = __ffsll((unsigned long long)todo) - 1;
-                const int at = i < nn ? a.pos[r0 + i] : -1;
-                if (i >= nn || !(at > pos - a.window || at < a.sinks)) left &= ~(1ull << i);
-            }
-            t.anc = left;
+        for (int ks = 0; ks < HD / 16; ks++)
+            sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kp + ks * 16), t.qf[ks], sc, 0, 0, 0);
+        const unsigned seen = seen_keys<HD>(a, s, t, here, kb, half);
+#pragma unroll 1
+        for (int tok = 0; tok < 32; tok++) {
+            const int at = ((tok >> 4) << 3) | (tok & 7), from = l32 + 32 * ((tok >> 3) & 1);
+            float own = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; e++) own = e == at ? sc[e] : own;
+            const float p = fast_exp2(__builtin_fmaf(__shfl(own, from), a.scale_log2, t.m == -INFINITY ? 0.f : -t.m));
+            const bool sees = (__shfl((int)seen, from) >> at) & 1;
+            const bf16_t* src = a.vc + ((size_t)max(tok < 16 ? here.p0 : here.p1, 0) * a.hkv + j) * 16 * HD + (tok & 15) + half * 64;
+#pragma unroll
+            for (int dt = 0; dt < HD / 32; dt++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) {
+                    const float x = bf16_to_f32(src[(dt * 32 + 8 * (e >> 2) + (e & 3)) * 16]);
+                    t.o[dt][e] = sees && !(fabsf(x) < INFINITY) ? t.o[dt][e] + p * x : t.o[dt][e];
+                }
         }
-        const int p = s.partition(c);
-        walk_keys<HD>(a, s, bt, j, s.skip(p * a.part_keys), min(s.total, (p + 1) * a.part_keys), all_lo, s.L, t, lane);
-        store_partial<HD>(t.o, t.m, t.l, a.part_o, a.part_ml, r0, rt, R, G, a.hq, j, a.max_parts, c, half, l32);
     }
 }
 
-// Joins the partitions of one (row, query head) in their order: one wavefront each, four per workgroup.
+// A partition's result for the lane's row, as store_partial leaves it (the running maximum and sum in fp32, the normalised output in fp16),
+// in pieces of 16 bytes: lanes l and l + 32, which hold dims 8 g .. 8 g + 3 and 8 g + 4 .. of a row, exchange halves, so that one has all eight
+// of an even g, the other of an odd one.  (Half as many stores in the middle of the key stream as in pieces of 8 bytes.)
 template <int HD>
+__device__ __forceinline__ void put_partial(const win_args& a, const row_tile<HD>& t, int r0, int rt, int R, int G, int j, int c, int lane) {
+    const int half = lane >> 5, rho = rt * 32 + (lane & 31);
+    const float inv = t.l > 0.f ? 1.f / t.l : 0.f;      // a partition in which the row sees no key: all zero
+    const int node = rho / G;
+    const size_t prow = ((size_t)(r0 + node) * a.hq + j * G + (rho - node * G)) * a.max_parts + c;
+    _Float16* po = a.part_o + prow * HD + 8 * half;
+#pragma unroll
+    for (int dt = 0; dt < HD / 32; dt++)
+#pragma unroll
+        for (int g = 0; g < 4; g += 2) {
+            unsigned x[4];      // (dims of g, of g + 1)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+                const f16x2 v = {(_Float16)(t.o[dt][4 * g + 2 * i] * inv), (_Float16)(t.o[dt][4 * g + 2 * i + 1] * inv)};
+                x[i] = __builtin_bit_cast(unsigned, v);
+            }
+            // the upper half of the first operand and the lower half of the second change places
+            const auto lo = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false), hi = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
+            if (rho < R) *reinterpret_cast<u32x4*>(po + dt * 32 + 8 * g) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+        }
+    if (half == 0 && rho < R) *reinterpret_cast<float2*>(a.part_ml + 2 * prow) = make_float2(t.m, t.l);
+}
+
+// A draft's row tile before its first key.
+template <int HD>
+__device__ __forceinline__ void begin_tile(row_tile<HD>& t) {
+#pragma unroll
+    for (int dt = 0; dt < HD / 32; dt++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) t.o[dt][e] = 0.f;
+    t.m = -INFINITY;
+    t.l = 0.f;
+}
+// Queries and visible keys of a draft's row tile.
+template <int HD>
+__device__ __forceinline__ void load_rows(const win_args& a, const win_span& s, int r0, int nn, int rt, int j, int all_lo, row_tile<HD>& t,
+                                          int lane) {
+    const int half = lane >> 5, l32 = lane & 31, G = a.hq / a.hkv, R = nn * G, rho = rt * 32 + l32;
+    load_query_tile<HD>(a.q, a.anc_mask, r0, rt, R, G, a.hq, j, half, l32, t.qf, t.anc);
+    const int pos = rho < R ? max(a.pos[r0 + rho / G], 0) : s.L;
+    t.lo = min(max(pos + 1 - a.window, s.first), all_lo);
+    t.hi = s.L;
+    if (a.window < HS_MAX_NODES) {
+        // ancestors that lie behind the window
+        uint64_t left = t.anc;
+        for (uint64_t todo = t.anc; todo; todo &= todo - 1) {
+            const int i = __ffsll((unsigned long long)todo) - 1;
+            const int at = i < nn ? a.pos[r0 + i] : -1;
+            if (i >= nn || !(at > pos - a.window || at < a.sinks)) left &= ~(1ull << i);
+        }
+        t.anc = left;
+    }
+}
+
+// Partitions c, c + step, ... of a (sequence, KV head) by one wavefront.
+template <int HD>
+__device__ __forceinline__ void walk_partitions(const win_args& a, const win_span& s, const int32_t* __restrict__ bt, int j, int r0, int nn,
+                                                int c, int step, int lane) {
+    const int half = lane >> 5, l32 = lane & 31, G = a.hq / a.hkv, R = nn * G;
+    // its depth is below nn, so that from all_lo on every row sees every cached key
+    const int all_lo = max(0, s.L + nn - a.window);
+    // (of a draft with more nodes than the limits allow there are more tiles, and more partitions)
+    for (; c < s.n_parts; c += step)
+        for (int rt = 0; rt * 32 < R; rt++) {
+            row_tile<HD> t;
+            load_rows<HD>(a, s, r0, nn, rt, j, all_lo, t, lane);
+            begin_tile<HD>(t);
+            const int p = s.partition(c);
+            const int k0 = s.skip(p * a.part_keys), k_end = min(s.total, (p + 1) * a.part_keys);
+            if (walk_keys<HD>(a, s, bt, j, k0, k_end, all_lo, s.L, t, lane)) add_odd<HD>(a, s, bt, j, k0, k_end, all_lo, s.L, t, lane);
+            put_partial<HD>(a, t, r0, rt, R, G, j, c, lane);
+        }
+}
+
+// Drafts of at most 32 query rows per KV head (plain decoding, as a rule): a wavefront per partition.
+template <int HD>
+__global__ __launch_bounds__(256, 2) void window_rows(win_args a) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
+    const int g = blockIdx.x % a.groups, pair = blockIdx.x / a.groups;
+    const int j = pair % a.hkv, b = pair / a.hkv;
+    const int r0 = a.row_off[b], nn = a.row_off[b + 1] - r0;
+    const int G = a.hq / a.hkv, R = nn * G;
+    const win_span s = make_span(a.seq_len[b], nn, a);
+    const int32_t* bt = a.block_table + (size_t)b * a.max_blocks;
+    walk_partitions<HD>(a, s, bt, j, r0, nn, 4 * g + wave, 4 * a.groups, lane);
+}
+
+// Drafts of any size.  A workgroup takes a run of partitions of a (sequence, KV head) with four row tiles, a wavefront each: one stream of
+// 32-key tiles through a ring in LDS that the wavefronts fill and read together, across partitions.  The keys come from memory once for all
+// rows, and three tiles of 16 KB are on their way at any time, which loads into registers have no room for.  A tile is a page's K or V^T block
+// per wavefront, straight into LDS (the layout: sub_tile).  One barrier per tile: it says that the tile has landed (every wavefront has waited
+// for its share) and that its predecessor has been read, whose place is refilled then.  (A sequence with one row tile keeps one wavefront
+// busy with products: two workgroups per compute unit are enough for the memory's pace.)
+// There are one or two groups of four tiles (at most 256 query rows per KV head); the workgroups of the second, most of which have nothing to do,
+// come last.  (In turn with the others, live and idle workgroups alternated on the way to the shader engines, and of two places on a compute unit
+// one stayed empty: 256 sequences with a long tail of lengths, 4096 keys, 28 heads, 600 us instead of 435.)
+constexpr int WIN_RING = 4, WIN_RUN = 512;      // tiles in LDS; of a run
+constexpr int WIN_START = 3;
+template <int HD>
+__global__ __launch_bounds__(256, 2) void window_rows_ring(win_args a, int tile_groups) {
+    using T = sub_tile<HD>;
+    constexpr int NKS = HD / 16, NDT = HD / 32, CPW = T::PAGE / 1024;   // 1 KB loads per wavefront and tile
+    static_assert(WIN_RING == 4, "the wait counts below");
+    __shared__ __attribute__((aligned(1024))) unsigned char ring[WIN_RING * T::BYTES];
+    __shared__ int s_page[2 * WIN_RUN];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
+    const int units = a.groups * a.hkv * a.batch, unit = blockIdx.x % units, group = blockIdx.x / units;
+    const int g = unit % a.groups, pair = unit / a.groups;
+    const int j = pair % a.hkv, b = pair / a.hkv;
+    const int r0 = a.row_off[b], nn = a.row_off[b + 1] - r0;
+    const int G = a.hq / a.hkv, R = nn * G, nrt = (R + 31) >> 5;
+    const win_span s = make_span(a.seq_len[b], nn, a);
+    const int32_t* bt = a.block_table + (size_t)b * a.max_blocks;
+    const int all_lo = max(0, s.L + nn - a.window);      // (see window_rows)
+    const int c_begin = (int)((long long)s.n_parts * g / a.groups), c_end = (int)((long long)s.n_parts * (g + 1) / a.groups);
+    if (4 * group >= nrt || c_begin >= c_end) return;
+
+    // the run's tiles: n_low of them from k0 on, and then from k1 on (behind the gap between sinks and window)
+    const int p_last = s.partition(c_end - 1);
+    const int k0 = s.skip(s.partition(c_begin) * a.part_keys), k_end = min(s.total, (p_last + 1) * a.part_keys);
+    const int k1 = s.first & ~31;
+    const int n_low = k0 < k1 ? (min(min(s.sink_end, k1), k_end) - k0 + 31) >> 5 : 0;
+    const int low_to = k0 < k1 ? k1 : k0;
+    const int n_tiles = n_low + max(0, (k_end - low_to + 31) >> 5);
+    auto key_of = [&](int i) { return i < n_low ? k0 + 32 * i : low_to + 32 * (i - n_low); };
+
+    // the wavefront's share of a tile: K (is_v = 0) or V^T of its page `pg`
+    const size_t page_bytes = (size_t)a.hkv * T::PAGE;
+    const int is_v = wave & 1, pg = wave >> 1;
+    const unsigned ring_off = (unsigned)(size_t)(hs_gemm_detail::lds_ptr_t)ring + is_v * T::V + pg * T::PAGE;
+    const unsigned char* base = reinterpret_cast<const unsigned char*>(is_v ? a.vc : a.kc) + (size_t)j * T::PAGE;
+    unsigned from[CPW];   // where in the page's block a lane's 16 bytes of load i come from
+#pragma unroll
+    for (int i = 0; i < CPW; i++) {
+        const int c = lane + 64 * i;
+        from[i] = is_v ? T::v_from(c) : T::k_at(c / (HD / 8), c % (HD / 8));   // (K's permutation is its own inverse)
+    }
+    const int key_row = (l32 & 16) | page_order(l32 & 15);
+
+    for (int i = tid; i < 2 * n_tiles; i += 256) {
+        const int p0 = key_of(i >> 1) + 16 * (i & 1), at = p0 >> 4;
+        int page = -1;
+        if (at < a.max_blocks && p0 < k_end && (p0 < s.sink_end || p0 + 16 > s.first)) page = bt[at];
+        s_page[i] = page < a.n_blocks ? page : -1;
+    }
+    // (one turn, but for a draft of more nodes than the launch provides for)
+    for (int tg = 4 * group; tg < nrt; tg += 4 * tile_groups) {
+        const int rt = tg + ((wave - g - j - b) & 3);      // (two of four wavefronts with rows are not the same two everywhere)
+        row_tile<HD> t;
+        load_rows<HD>(a, s, r0, nn, rt, j, all_lo, t, lane);
+        begin_tile<HD>(t);
+        // (waited for here: inside the loop the wait would be for every load in flight)
+#pragma unroll
+        for (int ks = 0; ks < NKS; ks++) asm volatile("" : "+v"(t.qf[ks]));
+        asm volatile("" : "+v"(t.anc), "+v"(t.lo));
+        __syncthreads();      // (the pages are there, the ring has been read)
+        auto page_of = [&](int i, int pp) { return __builtin_amdgcn_readfirstlane(s_page[2 * i + pp]); };
+        int ahead = 0, f = 0, f_slot = 0, f_page = page_of(0, pg);      // ahead: tiles asked for and not yet waited for
+        auto fetch = [&]() __attribute__((always_inline)) {
+            const unsigned char* src = base + (size_t)max(f_page, 0) * page_bytes;
+            const unsigned dst = ring_off + f_slot * T::BYTES;
+#pragma unroll
+            for (int i = 0; i < CPW; i++) hs_gemm_detail::load_to_lds_16_stream(src, from[i], dst + i * 1024);
+            f_slot = (f_slot + 1) & (WIN_RING - 1);
+            ahead++;
+            if (++f < n_tiles) f_page = page_of(f, pg);
+        };
+        // waits for the wavefront's own part of the tile at the head of what it asked for, then for everybody's
+        auto landed = [&](bool take_one) __attribute__((always_inline)) {
+            if (take_one) {
+                ahead--;
+                if (ahead >= 2) HS_WAIT_VMCNT(2 * CPW);
+                else if (ahead == 1) HS_WAIT_VMCNT(CPW);
+                else HS_WAIT_VMCNT(0);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        };
+        auto load_keys = [&](int slot, key_tile<HD>& k) __attribute__((always_inline)) {
+            int at = T::k_at(key_row, half);       // (chunk 2 ks + half: the permutation is an exclusive or, and so is 2 ks)
+            asm volatile("" : "+v"(at));
+            const unsigned char* tile = ring + slot * T::BYTES;
+#pragma unroll
+            for (int ks = 0; ks < NKS; ks++) k.k[ks] = *reinterpret_cast<const bf16x8*>(tile + (at ^ (ks << 5)));
+        };
+        auto scores = [&](const key_tile<HD>& k) __attribute__((always_inline)) {
+            f32x16 sc;
+#pragma unroll
+            for (int e = 0; e < 16; e++) sc[e] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < NKS; ks++) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.k[ks], t.qf[ks], sc, 0, 0, 0);
+            return sc;
+        };
+        while (ahead < WIN_RING - 1 && f < n_tiles) fetch();
+        landed(!is_v);      // the first keys
+        if (ahead < WIN_RING - 1 && f < n_tiles) fetch();
+        if (rt >= nrt) {
+            // (no rows: only its share of the tiles)
+            for (int i = 0; i < n_tiles; i++) {
+                landed(is_v || i + 1 < n_tiles);
+                if (ahead < WIN_RING - 1 && f < n_tiles) fetch();
+            }
+            continue;
+        }
+        // The keys run one tile ahead of the values, so that the next tile's first product is issued between this one's exponentials.
+        int slot = 0, c = c_begin, k_next = (s.partition(c) + 1) * a.part_keys, k_first = k0;
+        bool odd = false;
+        f32x16 sc;
+        {
+            key_tile<HD> k;
+            load_keys(0, k);
+            sc = scores(k);
+        }
+        for (int i = 0; i < n_tiles; i++) {
+            landed(is_v || i + 1 < n_tiles);      // this tile's values, the next one's keys
+            if (ahead < WIN_RING - 1 && f < n_tiles) fetch();
+            const int kb = key_of(i), after = key_of(i + 1);
+            key_tile<HD> k;
+            value_tile<HD> v;
+            const places here = {page_of(i, 0), page_of(i, 1)};
+            load_keys((slot + 1) & (WIN_RING - 1), k);       // (of the last tile: of whatever lies there, not used)
+            const bool masked = tile_masked(a, here, kb, all_lo, s.L);
+            const float alpha = take_scores<HD>(a, s, t, sc, here, masked, kb, half);
+            // (only here: with the keys, the values and the masks at the same time the registers would not do)
+#pragma unroll
+            for (int pp = 0; pp < 2; pp++)
+#pragma unroll
+                for (int dt = 0; dt < NDT; dt++)
+                    v.v[pp][dt] = *reinterpret_cast<const bf16x8*>(ring + slot * T::BYTES + T::V + pp * T::PAGE + dt * 1024 + T::v_at(l32, half));
+            if (masked) odd |= mask_values<HD>(v);
+            bf16x8 pb[2];
+            const f32x16 next = scores(k);
+            take_probabilities<HD>(a, t, sc, alpha, pb);
+            take_values<HD>(t, v, pb);
+#pragma unroll
+            for (int q = 0; q < NKS; q++) {             // a product, its share of the exponentials
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x402, 64 / NKS, 0);
+            }
+            sc = next;
+            slot = (slot + 1) & (WIN_RING - 1);
+            if (i + 1 == n_tiles || after >= k_next) {
+                if (__any(odd)) {
+                    add_odd<HD>(a, s, bt, j, k_first, min(k_end, k_next), all_lo, s.L, t, lane);
+                    odd = false;
+                }
+                put_partial<HD>(a, t, r0, rt, R, G, j, c, lane);
+                begin_tile<HD>(t);
+                c++;
+                k_next = (s.partition(c) + 1) * a.part_keys;
+                k_first = after;
+            }
+        }
+    }
+}
+
+// Joins the partitions of a row's query heads in their order: a wavefront takes 512 / HD heads of a row, a lane eight elements of one.  Eight
+// partitions at a time, all of which are asked for before the first is used; more than eight (in steps of eight) move the maximum as a
+// softmax over the keys does.  EARLY: with few rows the first eight are asked for before it is known how many there are, and whether there is
+// the row: what a launch of a few rows takes is its chain of round trips to memory (count, row's sequence, its length, partial results).
+template <int HD, bool EARLY>
 __global__ __launch_bounds__(256) void window_merge(win_args a) {
-    constexpr int E = HD / 64;
-    typedef _Float16 piece __attribute__((ext_vector_type(E)));
-    const int head = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (head >= a.hq) return;
-    const int M = a.row_off[a.batch];
-    for (int row = blockIdx.x; row < M; row += gridDim.x) {
+    constexpr int LANES = HD / 8, HEADS = 64 / LANES, AHEAD = 8;
+    typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+    const int lane = threadIdx.x & 63, head = (blockIdx.y * 4 + (threadIdx.x >> 6)) * HEADS + lane / LANES;
+    if ((blockIdx.y * 4 + (threadIdx.x >> 6)) * HEADS >= a.hq) return;
+    for (int row = blockIdx.x;; row += gridDim.x) {
+        const size_t prow = ((size_t)row * a.hq + min(head, a.hq - 1)) * a.max_parts;
+        const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + prow;
+        const _Float16* po = a.part_o + prow * HD + 8 * (lane % LANES);
+        float2 x0[AHEAD];
+        f16x8 v0[AHEAD];
+        if constexpr (EARLY) {
+            // (in bounds whether the row and its partitions exist or not: the grid is no larger than the workspace's rows)
+#pragma unroll
+            for (int p = 0; p < AHEAD; p++) {
+                x0[p] = ml[min(p, a.max_parts - 1)];
+                v0[p] = *reinterpret_cast<const f16x8*>(po + (size_t)min(p, a.max_parts - 1) * HD);
+            }
+            hs_loads_issued();
+        }
+        if (row >= a.row_off[a.batch]) return;
         const int b = a.row2seq[row];
         const int n = make_span(a.seq_len[b], a.row_off[b + 1] - a.row_off[b], a).n_parts;
-        const size_t prow = ((size_t)row * a.hq + head) * a.max_parts;
-        const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + prow;
-        const _Float16* po = a.part_o + prow * HD + E * lane;
-        float top = -INFINITY;
-        for (int p = lane; p < n; p += 64) top = fmaxf(top, ml[p].x);
+        float top = -INFINITY, den = 0.f, acc[8];
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-        float den = 0.f, acc[E];
+        for (int i = 0; i < 8; i++) acc[i] = 0.f;
+        for (int p0 = 0; p0 < n; p0 += AHEAD) {
+            float2 x[AHEAD];
+            f16x8 v[AHEAD];
 #pragma unroll
-        for (int i = 0; i < E; i++) acc[i] = 0.f;
-        for (int p = 0; p < n; p++) {
-            const float2 x = ml[p];
-            // the partition's weight in the whole; its output is stored normalised
-            const float w = x.x == -INFINITY ? 0.f * x.y : fast_exp2(x.x - top) * x.y;
-            const piece v = *reinterpret_cast<const piece*>(po + (size_t)p * HD);
-            den += w;
+            for (int p = 0; p < AHEAD; p++) {
+                const int at = min(p0 + p, n - 1);
+                if (EARLY && p0 == 0) {
+                    x[p] = p < n ? x0[p] : make_float2(-INFINITY, 0.f);
+                    v[p] = v0[p];
+                } else {
+                    x[p] = ml[at];
+                    v[p] = *reinterpret_cast<const f16x8*>(po + (size_t)at * HD);
+                }
+            }
+            float m = top;
 #pragma unroll
-            for (int i = 0; i < E; i++) acc[i] += w * (float)v[i];
+            for (int p = 0; p < AHEAD; p++) m = fmaxf(m, x[p].x);
+            const float safe = m == -INFINITY ? 0.f : m;
+            if (p0 > 0) {
+                const float alpha = fast_exp2(top - safe);
+                den *= alpha;
+#pragma unroll
+                for (int i = 0; i < 8; i++) acc[i] *= alpha;
+            }
+            top = m;
+#pragma unroll
+            for (int p = 0; p < AHEAD; p++) {
+                if (p0 + p >= n) break;
+                // the partition's weight in the whole; its output is stored normalised
+                const float w = fast_exp2(x[p].x - safe) * x[p].y;
+                den += w;
+#pragma unroll
+                for (int i = 0; i < 8; i++) acc[i] += w * (float)v[p][i];
+            }
         }
-        bf16_t* dst = a.out + ((size_t)row * a.hq + head) * HD + E * lane;
+        if (head < a.hq) {
+            const float inv = den == 0.f ? 0.f : 1.f / den;
+            u32x4 y;
 #pragma unroll
-        for (int i = 0; i < E; i++) dst[i] = f32_to_bf16(den == 0.f ? 0.f : acc[i] / den);
+            for (int i = 0; i < 4; i++) y[i] = (uint32_t)to_bf16(acc[2 * i] * inv) | ((uint32_t)to_bf16(acc[2 * i + 1] * inv) << 16);
+            *reinterpret_cast<u32x4*>(a.out + ((size_t)row * a.hq + head) * HD + 8 * (lane % LANES)) = y;
+        }
     }
 }
 
@@ -326,12 +644,7 @@ __global__ __launch_bounds__(256, 2) void window_chunk(win_args a, int nx) {
     for (int rt = (blockIdx.x % nx) * 4 + wave; rt * 32 < R; rt += nx * 4) {
         row_tile<HD> t;
         load_query_tile<HD>(a.q, nullptr, r0, rt, R, G, a.hq, j, half, l32, t.qf, t.anc);
-#pragma unroll
-        for (int dt = 0; dt < HD / 32; dt++)
-#pragma unroll
-            for (int e = 0; e < 16; e++) t.o[dt][e] = 0.f;
-        t.m = -INFINITY;
-        t.l = 0.f;
+        begin_tile<HD>(t);
         const int rho = rt * 32 + l32;
         const int node0 = rt * 32 / G, node1 = min(nn - 1, (rt * 32 + 31) / G), node = min(rho / G, nn - 1);
         t.lo = max(0, s.L + node + 1 - a.window);
@@ -339,8 +652,8 @@ __global__ __launch_bounds__(256, 2) void window_chunk(win_args a, int nx) {
         win_span w = s;     // the keys of this tile's rows
         w.first = max(0, s.L + node0 + 1 - a.window);
         w.sink_end = min(min(a.sinks, w.first), s.total);
-        walk_keys<HD>(a, w, bt, j, w.skip(0), min(s.total, s.L + node1 + 1), max(0, s.L + node1 + 1 - a.window), s.L + node0 + 1, t,
-                      lane);
+        const int k0 = w.skip(0), k_end = min(s.total, s.L + node1 + 1), all_lo = max(0, s.L + node1 + 1 - a.window), all_hi = s.L + node0 + 1;
+        if (walk_keys<HD>(a, w, bt, j, k0, k_end, all_lo, all_hi, t, lane)) add_odd<HD>(a, w, bt, j, k0, k_end, all_lo, all_hi, t, lane);
         if (rho >= R) continue;
         const float inv = t.l == 0.f ? 0.f : 1.f / t.l;
         bf16_t* po = a.out + ((size_t)(r0 + node) * a.hq + j * G + (rho - node * G)) * HD;
@@ -349,12 +662,15 @@ __global__ __launch_bounds__(256, 2) void window_chunk(win_args a, int nx) {
 #pragma unroll
             for (int g4 = 0; g4 < 4; g4++) {
                 u32x2 x;
-                x.x = (uint32_t)f32_to_bf16(t.o[dt][4 * g4] * inv) | ((uint32_t)f32_to_bf16(t.o[dt][4 * g4 + 1] * inv) << 16);
-                x.y = (uint32_t)f32_to_bf16(t.o[dt][4 * g4 + 2] * inv) | ((uint32_t)f32_to_bf16(t.o[dt][4 * g4 + 3] * inv) << 16);
+                x.x = (uint32_t)to_bf16(t.o[dt][4 * g4] * inv) | ((uint32_t)to_bf16(t.o[dt][4 * g4 + 1] * inv) << 16);
+                x.y = (uint32_t)to_bf16(t.o[dt][4 * g4 + 2] * inv) | ((uint32_t)to_bf16(t.o[dt][4 * g4 + 3] * inv) << 16);
                 *reinterpret_cast<u32x2*>(po + dt * 32 + 8 * g4 + 4 * half) = x;
             }
     }
 }
+
+// The most query rows per KV head that a draft can have.
+int rows_of(const hs_ctx* ctx) { return ctx->desc.n_q_heads / ctx->desc.n_kv_heads * (1 + ctx->lim.c_max * ctx->lim.k_max); }
 
 // Partitions of a draft's keys: their length, and the most that a sequence can have.  A function of the context's limits, the window
 // and the sinks, so that the order of a row's sums is the same in every step.
@@ -365,8 +681,11 @@ win_plan plan_rows(const hs_ctx* ctx, int window, int sinks) {
     auto most = [&](long long part) {
         return std::min((s + part - 1) / part + (span + nodes - 2) / part + 2, (cap + part - 1) / part);
     };
-    long long part = 1024;
-    while (part > 64 && (long long)ctx->lim.max_batch * ctx->desc.n_kv_heads * ((span + part - 1) / part) < 2048) part /= 2;
+    // Long partitions mean fewer partial results, which are written into the middle of the key stream; short ones keep a small batch spread
+    // over the chip: a wavefront each of a draft of few rows, a workgroup each of larger ones.
+    const bool wave = rows_of(ctx) <= 32;
+    long long part = wave ? 1024 : 2048;
+    while (part > 64 && (long long)ctx->lim.max_batch * ctx->desc.n_kv_heads * ((span + part - 1) / part) < (wave ? 2048 : 512)) part /= 2;
     while (part < ctx->att_part && most(part) > ctx->max_parts) part *= 2;      // (what the workspace holds)
     if (most(part) > ctx->max_parts) part = ctx->att_part;
     return {(int)part, (int)most(part)};
@@ -407,18 +726,45 @@ win_args make_args(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const
 
 void hs_launch_window_attention(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step,
                                 const void* q, void* out, int window, int sinks, hipStream_t st) {
-    const win_args a = make_args(ctx, layer, cache, seq, step, q, out, window, sinks);
-    const dim3 grid((unsigned)((a.max_parts + 3) / 4 * a.hkv * a.batch));
-    if (ctx->desc.head_dim == 128) hipLaunchKernelGGL((window_rows<128>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((window_rows<64>), grid, dim3(256), 0, st, a);
+    win_args a = make_args(ctx, layer, cache, seq, step, q, out, window, sinks);
+    const int most = rows_of(ctx);
+    if (most <= 32) {
+        a.groups = (a.max_parts + 3) / 4;
+        const dim3 grid((unsigned)(a.groups * a.hkv * a.batch));
+        if (ctx->desc.head_dim == 128) hipLaunchKernelGGL((window_rows<128>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((window_rows<64>), grid, dim3(256), 0, st, a);
+        return;
+    }
+    // How many workgroups share the partitions of a (sequence, KV head): as many as make the fewest tiles one after the other, in
+    // rounds of two workgroups per compute unit, of which each takes as long as WIN_START tiles until its first one is there.  (Its page
+    // numbers have to fit in LDS.)
+    const int tile_groups = (most + 127) / 128;
+    long long best = 0;
+    for (int groups = 1; groups <= a.max_parts; groups++) {
+        const int run = (a.max_parts + groups - 1) / groups * (a.part_keys / 32);
+        if (run > WIN_RUN) continue;
+        const long long rounds = ((long long)groups * a.hkv * a.batch + 2 * ctx->n_cu - 1) / (2 * ctx->n_cu);
+        const long long cost = rounds * (WIN_START + run);
+        if (a.groups == 0 || cost < best) { best = cost; a.groups = groups; }
+    }
+    const dim3 grid((unsigned)(a.groups * a.hkv * a.batch * tile_groups));
+    if (ctx->desc.head_dim == 128) hipLaunchKernelGGL((window_rows_ring<128>), grid, dim3(256), 0, st, a, tile_groups);
+    else hipLaunchKernelGGL((window_rows_ring<64>), grid, dim3(256), 0, st, a, tile_groups);
 }
 
 void hs_launch_window_merge(const hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step, void* out,
                             int window, int sinks, hipStream_t st) {
     const win_args a = make_args(ctx, 0, cache, seq, step, nullptr, out, window, sinks);
-    const dim3 grid(hs_row_grid(ctx, 256, (a.hq + 3) / 4), (a.hq + 3) / 4);
-    if (ctx->desc.head_dim == 128) hipLaunchKernelGGL((window_merge<128>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((window_merge<64>), grid, dim3(256), 0, st, a);
+    const int per = 4 * 512 / ctx->desc.head_dim, sets = (a.hq + per - 1) / per;      // heads of a workgroup, workgroups of a row
+    const dim3 grid(hs_row_grid(ctx, 256, sets), sets);
+    const bool early = ctx->lim.max_rows <= HS_EARLY_ROWS;
+    if (ctx->desc.head_dim == 128) {
+        if (early) hipLaunchKernelGGL((window_merge<128, true>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((window_merge<128, false>), grid, dim3(256), 0, st, a);
+    } else {
+        if (early) hipLaunchKernelGGL((window_merge<64, true>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((window_merge<64, false>), grid, dim3(256), 0, st, a);
+    }
 }
 
 void hs_launch_window_chunk(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const hs_seq_state* seq, const int32_t* len_plus1,
