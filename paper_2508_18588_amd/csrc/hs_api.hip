@@ -59,6 +59,8 @@ void layout_workspace(hs_ctx* ctx) {
     w.reject_walk = take((size_t)l.max_batch * 16);
     w.reject_stats = take(M * (size_t)hs_reject_slices(d.vocab) * sizeof(hs_reject_stat));
     w.probs_sums = take((size_t)HS_PROBS_ROUNDS * l.max_batch * hs_probs_slices(d.vocab) * sizeof(double));
+    w.probs_records = take((size_t)HS_PROBS_ROUNDS * l.max_batch * HS_PROBS_RECORD);
+    w.probs_stats = take(HS_PROBS_STATS * 8);
     w.total = off;
 }
 

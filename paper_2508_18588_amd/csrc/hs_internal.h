@@ -27,11 +27,13 @@ static inline int hs_reject_slices(int vocab) { return (vocab + HS_REJECT_SLICE 
 
 // Verification against probabilities: the vocabulary is summed in slices of this many tokens, for each sequence in up to
 // HS_PROBS_ROUNDS launches.
-constexpr int HS_PROBS_SLICE = 4096, HS_PROBS_ROUNDS = 2;
+constexpr int HS_PROBS_SLICE = 4096, HS_PROBS_ROUNDS = 2, HS_PROBS_RECORD = 1536;      // (bytes of a walk's record)
+// Softmax of logits: rows of up to so many bytes are read twice by two launches, with a maximum and a sum for each of so many slices.
+constexpr size_t HS_PROBS_CACHED = 192u << 20, HS_PROBS_STATS = 32768;
 static inline int hs_probs_slices(int vocab) { return (vocab + HS_PROBS_SLICE - 1) / HS_PROBS_SLICE; }
 
 struct hs_workspace_layout {
-    size_t x, xn, qkv, q, attn, act, part_o, part_ml, logits, logits_bytes, rowmax, draft_best, gemm_part, gemm_part_bytes, err, pf_len, row_info, att_work, att_list, reject_stats, reject_walk, probs_sums, total;
+    size_t x, xn, qkv, q, attn, act, part_o, part_ml, logits, logits_bytes, rowmax, draft_best, gemm_part, gemm_part_bytes, err, pf_len, row_info, att_work, att_list, reject_stats, reject_walk, probs_sums, probs_records, probs_stats, total;
 };
 
 struct hs_ctx {

@@ -13,15 +13,79 @@ __device__ __forceinline__ float wide(bf16_t v) { return bf16_to_f32(v); }
 __device__ __forceinline__ void narrow(float v, float& to) { to = v; }
 __device__ __forceinline__ void narrow(float v, bf16_t& to) { to = __builtin_isnan(v) ? (bf16_t)0x7FC0 : f32_to_bf16(v); }
 
-// ---- p[t] = exp((l[t] - max l) / T) / sum: one workgroup per row, two passes over it.
+// Eight tokens from i on, as 32-bit values; `rest` beyond the row's n.  whole: 16-byte accesses are possible (i is a multiple of eight).
+// (Stores are non-temporal: what they would take of the caches is better used by logits that are read again, 390 -> 357 us for 1088 rows of
+// 152064 tokens when a workgroup read all of its row twice.)
+constexpr int PIECE = 8;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void load_piece(const float* __restrict__ row, int i, int n, bool whole, float rest, float (&v)[PIECE]) {
+    if (whole && i + PIECE <= n) {
+#pragma unroll
+        for (int e = 0; e < PIECE; e += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(row + i + e);
+            v[e] = x.x; v[e + 1] = x.y; v[e + 2] = x.z; v[e + 3] = x.w;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < PIECE; e++) v[e] = i + e < n ? row[i + e] : rest;
+    }
+}
+__device__ __forceinline__ void load_piece(const bf16_t* __restrict__ row, int i, int n, bool whole, float rest, float (&v)[PIECE]) {
+    if (whole && i + PIECE <= n) {
+        const uint4 x = *reinterpret_cast<const uint4*>(row + i);
+        const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int e = 0; e < PIECE; e += 2) {
+            v[e] = __uint_as_float(u[e / 2] << 16);
+            v[e + 1] = __uint_as_float(u[e / 2] & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < PIECE; e++) v[e] = i + e < n ? wide(row[i + e]) : rest;
+    }
+}
+__device__ __forceinline__ void store_piece(float* __restrict__ row, int i, int n, bool whole, const float (&v)[PIECE]) {
+    if (whole && i + PIECE <= n) {
+#pragma unroll
+        for (int e = 0; e < PIECE; e += 4) __builtin_nontemporal_store(f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]}, reinterpret_cast<f32x4*>(row + i + e));
+    } else {
+#pragma unroll
+        for (int e = 0; e < PIECE; e++)
+            if (i + e < n) row[i + e] = v[e];
+    }
+}
+__device__ __forceinline__ void store_piece(bf16_t* __restrict__ row, int i, int n, bool whole, const float (&v)[PIECE]) {
+    bf16_t b[PIECE];
+#pragma unroll
+    for (int e = 0; e < PIECE; e++) narrow(v[e], b[e]);
+    if (whole && i + PIECE <= n) {
+        u32x4 u;
+#pragma unroll
+        for (int e = 0; e < 4; e++) u[e] = (uint32_t)b[2 * e] | (uint32_t)b[2 * e + 1] << 16;
+        __builtin_nontemporal_store(u, reinterpret_cast<u32x4*>(row + i));
+    } else {
+#pragma unroll
+        for (int e = 0; e < PIECE; e++)
+            if (i + e < n) row[i + e] = b[e];
+    }
+}
+template <typename T>
+__device__ __forceinline__ bool whole_pieces(const void* p, size_t stride) {
+    return (((unsigned long long)p | stride * sizeof(T)) & 15ull) == 0;
+}
+
+// ---- p[t] = exp((l[t] - max l) / T) / sum.  Bound by memory: the logits once and the probabilities once, and of the second reading of the
+// logits, when maximum and sum are known, what the caches don't have.
 
 struct probs_args {
     const void* logits;
     void* out;
     size_t logits_stride, out_stride;
     const int32_t* live;      // rows that there are, or null: all
-    int rows, vocab;
+    int rows, vocab, n_slices, first;      // first: the number of row 0 in what live counts
     float c_hi, c_lo;         // log2(e) / T
+    float2* stats;            // [rows][n_slices]: largest logit and sum of a slice
 };
 
 // exp((l - m) / T): the exponent is a product of two parts, so that it is as exact as its result (a product rounded once is off by
@@ -32,23 +96,47 @@ __device__ __forceinline__ float weight(float l, float m, float c_hi, float c_lo
     // (an excluded logit at an infinite temperature; an exponent whose second part has lost its meaning)
     return d == -INFINITY || hi < -160.f ? 0.f : __builtin_fmaf(e * 0.6931471805599453f, lo, e);
 }
+// The sum of a thread's weights so far, relative to its largest logit, takes a piece.
+__device__ __forceinline__ void add_piece(const float (&v)[PIECE], const probs_args& p, float& m, float& s) {
+    float top = m;
+#pragma unroll
+    for (int e = 0; e < PIECE; e++) top = fmaxf(top, v[e]);
+    if (top != m) {
+        s *= weight(m, top, p.c_hi, p.c_lo);
+        m = top;
+    }
+#pragma unroll
+    for (int e = 0; e < PIECE; e++) s += v[e] == -INFINITY ? 0.f : weight(v[e], m, p.c_hi, p.c_lo);
+}
+__device__ __forceinline__ void normalise(float (&v)[PIECE], const probs_args& p, float top, float inv) {
+#pragma unroll
+    for (int e = 0; e < PIECE; e++) v[e] = (v[e] == -INFINITY ? 0.f : weight(v[e], top, p.c_hi, p.c_lo)) * inv;
+}
+__device__ __forceinline__ float wave_sum_f32(float v) {
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) v += __shfl_xor(v, k);
+    return v;
+}
 
+// Many rows: a workgroup each, which takes its second pass from the row's end to its start, the last part first that the caches still have.
+// One workgroup per compute unit, so that the rows at hand (256 of 608 KB) stay in the 256 MB of the last cache.  (With 57344 tokens in registers
+// and 32768 in LDS between the passes 1088 rows took 381 us instead of 357: the caches are good enough, and the wavefronts are better off.)
 template <typename TI, typename TO>
 __global__ __launch_bounds__(1024) void probs_rows(probs_args p) {
     __shared__ float red_m[16], red_s[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int M = p.live ? min(*p.live, p.rows) : p.rows;
+    const int M = p.live ? min(*p.live, p.rows) : p.rows, pieces = (p.vocab + PIECE - 1) / PIECE;
+    const bool in_whole = whole_pieces<TI>(p.logits, p.logits_stride), out_whole = whole_pieces<TO>(p.out, p.out_stride);
     for (int row = blockIdx.x; row < M; row += gridDim.x) {
         const TI* l = (const TI*)p.logits + row * p.logits_stride;
         TO* o = (TO*)p.out + row * p.out_stride;
         float m = -INFINITY, s = 0.f;
-        for (int i = tid; i < p.vocab; i += 1024) {
-            const float x = wide(l[i]);
-            if (x > m) {
-                s *= weight(m, x, p.c_hi, p.c_lo);
-                m = x;
-            }
-            s += x == -INFINITY ? 0.f : weight(x, m, p.c_hi, p.c_lo);
+        for (int q = tid; q < pieces; q += 2048) {
+            float v[2][PIECE];
+#pragma unroll
+            for (int u = 0; u < 2; u++) load_piece(l, (q + 1024 * u) * PIECE, p.vocab, in_whole, -INFINITY, v[u]);
+#pragma unroll
+            for (int u = 0; u < 2; u++) add_piece(v[u], p, m, s);
         }
         float top = wave_max_f32(m);
         __syncthreads();      // (the row before has been read)
@@ -57,19 +145,70 @@ __global__ __launch_bounds__(1024) void probs_rows(probs_args p) {
         top = red_m[0];
 #pragma unroll
         for (int w = 1; w < 16; w++) top = fmaxf(top, red_m[w]);
-        s = m == -INFINITY ? s : s * weight(m, top, p.c_hi, p.c_lo);
-#pragma unroll
-        for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
+        s = wave_sum_f32(m == -INFINITY ? s : s * weight(m, top, p.c_hi, p.c_lo));
         if (lane == 0) red_s[wave] = s;
         __syncthreads();
         float sum = 0.f;
 #pragma unroll
         for (int w = 0; w < 16; w++) sum += red_s[w];
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        for (int i = tid; i < p.vocab; i += 1024) {
-            const float x = wide(l[i]);
-            narrow(top == -INFINITY && x == -INFINITY ? 0.f : weight(x, top, p.c_hi, p.c_lo) * inv, o[i]);
+        for (int q = tid + (pieces - 1) / 2048 * 2048; q >= 0; q -= 2048) {
+            float v[2][PIECE];
+#pragma unroll
+            for (int u = 0; u < 2; u++) load_piece(l, (q + 1024 * u) * PIECE, p.vocab, in_whole, -INFINITY, v[u]);
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                normalise(v[u], p, top, inv);
+                store_piece(o, (q + 1024 * u) * PIECE, p.vocab, out_whole, v[u]);
+            }
         }
+    }
+}
+
+// Few rows: slices of 4096 tokens, a workgroup of 256 threads each; one launch for the slices' maxima and sums, one that joins them and writes.
+constexpr int PROBS_SLICE = 4096;
+template <typename TI>
+__global__ __launch_bounds__(256) void probs_stats(probs_args p) {
+    __shared__ float red_m[4], red_s[4];
+    const int slice = blockIdx.x % p.n_slices, row = blockIdx.x / p.n_slices, tid = threadIdx.x, wave = tid >> 6;
+    const TI* l = (const TI*)p.logits + row * p.logits_stride;
+    const bool whole = whole_pieces<TI>(p.logits, p.logits_stride);
+    float v[2][PIECE], m = -INFINITY, s = 0.f;
+    if (p.live && p.first + row >= *p.live) return;
+#pragma unroll
+    for (int u = 0; u < 2; u++) load_piece(l, slice * PROBS_SLICE + (tid + 256 * u) * PIECE, p.vocab, whole, -INFINITY, v[u]);
+#pragma unroll
+    for (int u = 0; u < 2; u++) add_piece(v[u], p, m, s);
+    const float top = block_max_f32(m, red_m);
+    s = wave_sum_f32(m == -INFINITY ? s : s * weight(m, top, p.c_hi, p.c_lo));
+    if ((tid & 63) == 0) red_s[wave] = s;
+    __syncthreads();
+    if (tid == 0) p.stats[(size_t)row * p.n_slices + slice] = make_float2(top, (red_s[0] + red_s[1]) + (red_s[2] + red_s[3]));
+}
+template <typename TI, typename TO>
+__global__ __launch_bounds__(256) void probs_write(probs_args p) {
+    const int slice = blockIdx.x % p.n_slices, row = blockIdx.x / p.n_slices, tid = threadIdx.x, lane = tid & 63;
+    const TI* l = (const TI*)p.logits + row * p.logits_stride;
+    TO* o = (TO*)p.out + row * p.out_stride;
+    const bool in_whole = whole_pieces<TI>(p.logits, p.logits_stride), out_whole = whole_pieces<TO>(p.out, p.out_stride);
+    float v[2][PIECE];
+    if (p.live && p.first + row >= *p.live) return;
+#pragma unroll
+    for (int u = 0; u < 2; u++) load_piece(l, slice * PROBS_SLICE + (tid + 256 * u) * PIECE, p.vocab, in_whole, -INFINITY, v[u]);
+    const float2* stats = p.stats + (size_t)row * p.n_slices;
+    float m = -INFINITY, s = 0.f;
+    for (int i = lane; i < p.n_slices; i += 64) m = fmaxf(m, stats[i].x);
+    const float top = wave_max_f32(m);
+    for (int i = lane; i < p.n_slices; i += 64) {
+        const float2 x = stats[i];
+        s += x.x == -INFINITY ? x.y : x.y * weight(x.x, top, p.c_hi, p.c_lo);
+    }
+    s = wave_sum_f32(s);
+    const float inv = s == 0.f ? 0.f : 1.f / s;
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+        normalise(v[u], p, top, inv);
+        store_piece(o, slice * PROBS_SLICE + (tid + 256 * u) * PIECE, p.vocab, out_whole, v[u]);
     }
 }
 
@@ -82,9 +221,11 @@ __global__ __launch_bounds__(1024) void probs_rows(probs_args p) {
 // The walk itself needs a few probabilities per node and no sums, unless a second child of a node is tried; what takes time is the sum over
 // the vocabulary at the node where it ends.  So the first launch lets every workgroup of a sequence walk for itself and then sum its
 // slice of the vocabulary; the last one walks again with the sums at hand and looks for the token.  A walk that needs the sum of a rejected
-// child's node on its way takes a further launch of the first kind; more of these than were launched are summed by the last one alone.
+// child's node on its way takes a further launch of the first kind; more of these than were launched are summed by the last one alone.  (Where
+// the walk has come to is recorded, so that the last launch need not walk again as a rule: a chain of round trips to memory less.)
 constexpr int SLICE = HS_PROBS_SLICE, PER = SLICE / 256;
 
+struct verify_record;
 struct verify_args {
     const int32_t *row_off, *tok, *parent;
     const void *p, *q;
@@ -92,6 +233,7 @@ struct verify_args {
     const float *u_accept, *u_sample;
     int batch, vocab, n_slices, k_stride, rounds;
     double* sums;      // [rounds][batch][n_slices]
+    verify_record* records;      // [rounds][batch]
     int32_t *accept_len, *n_out, *out_tok, *path_row;
 };
 
@@ -119,8 +261,9 @@ __device__ __forceinline__ verify_nodes load_nodes(const verify_args& a, int r0,
     return n;
 }
 
+// (the lane is the same for the whole wavefront: no trip through the LDS unit, of which a walk would make a dozen per node)
 __device__ __forceinline__ double from_lane(double v, int lane) {
-    return __hiloint2double(__shfl(__double2hiint(v), lane), __shfl(__double2loint(v), lane));
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
 }
 
 // Where a walk has come to: node cur after a accepted tokens and r rejected ones there.  Lane k < r: the k-th one (rej) and the sum that it
@@ -130,12 +273,13 @@ struct verify_walk {
     int cur, a, r, rej, path, out, ask;
     double z;
     bool done;      // that sum is known, and the walk has ended
+    bool last;      // it is the sum that the sample is drawn from
 };
 // total(i): the i-th sum that the walk asked for, of which `known` are there.
 template <typename Total>
 __device__ __forceinline__ verify_walk walk_drafts(const verify_nodes& n, int nn, int k_stride, bool point, int known, Total total,
                                                    int lane) {
-    verify_walk s = {0, 0, 0, -1, 0, 0, 0, 1.0, false};
+    verify_walk s = {0, 0, 0, -1, 0, 0, 0, 1.0, false, false};
     double w = n.w;
     unsigned long long tried = 0;
     for (;;) {
@@ -147,7 +291,7 @@ __device__ __forceinline__ verify_walk walk_drafts(const verify_nodes& n, int nn
             if (s.ask >= known) return s;
             z = total(s.ask++);
         }
-        const int t = __shfl(n.tok, c);
+        const int t = __builtin_amdgcn_readlane(n.tok, c);
         if (from_lane(n.u, c) * z * from_lane(n.q, c) < from_lane(w, c)) {
             if (lane == s.a) s.out = t;
             s.cur = c;
@@ -162,6 +306,7 @@ __device__ __forceinline__ verify_walk walk_drafts(const verify_nodes& n, int nn
             s.r++;
         }
     }
+    s.last = true;
     if (s.ask >= known) return s;
     if (!(total(s.ask) > 0.0)) {      // nothing is left: the sample is the target's own
         s.r = 0;
@@ -171,66 +316,48 @@ __device__ __forceinline__ verify_walk walk_drafts(const verify_nodes& n, int nn
     return s;
 }
 
-// The 16 tokens of a slice that are thread tid's, in 16-byte pieces where rows allow them; token(j) is the j-th one's number.
-template <typename T>
-__device__ __forceinline__ int slice_token(int slice, int j, bool vec) {
-    constexpr int N = 16 / sizeof(T);
-    return slice * SLICE + (vec ? N * ((int)threadIdx.x + 256 * (j / N)) + j % N : (int)threadIdx.x + 256 * j);
-}
-template <typename T>
-__device__ __forceinline__ void load_tokens(const T* __restrict__ row, int vocab, int slice, bool vec, float (&v)[PER]) {
-    constexpr int N = 16 / sizeof(T);
-    if (vec) {
-#pragma unroll
-        for (int j = 0; j < PER; j += N) {
-            const int i = slice_token<T>(slice, j, true);
-            union { uint4 u; T t[N]; } x;
-            x.u = make_uint4(0u, 0u, 0u, 0u);
-            if (i + N <= vocab) x.u = *reinterpret_cast<const uint4*>(row + i);
-            else {
-#pragma unroll
-                for (int e = 0; e < N; e++)
-                    if (i + e < vocab) x.t[e] = row[i + e];
-            }
-#pragma unroll
-            for (int e = 0; e < N; e++) v[j + e] = wide(x.t[e]);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < PER; j++) {
-            const int i = slice_token<T>(slice, j, false);
-            v[j] = i < vocab ? wide(row[i]) : 0.f;
-        }
-    }
-}
-template <typename T>
-__device__ __forceinline__ bool whole_pieces(const void* p, size_t stride) {
-    return (((unsigned long long)p | stride * sizeof(T)) & 15ull) == 0;
-}
-
-// What is left of a token's weight after r rejections.
-__device__ __forceinline__ double weight_left(double w, double q, int token, int r, const double* z, const int* rej, bool point) {
-    for (int k = 0; k < r; k++) w = point ? (rej[k] == token ? 0.0 : w) : fmax(w - z[k] * q, 0.0);
-    return w;
-}
-
 struct verify_left { double z[HS_MAX_NODES]; int rej[HS_MAX_NODES]; };
 __device__ __forceinline__ void publish(const verify_walk& s, verify_left& l, int tid) {      // by the first wavefront, whose walk it is
     if (tid < HS_MAX_NODES) { l.z[tid] = s.z; l.rej[tid] = s.rej; }
 }
+// Where the walk of a round has come to, for the kernel that picks the token: what is there says that it need not walk for itself.
+enum { RECORD_MORE = 0, RECORD_LAST = 1, RECORD_BEFORE = 2 };      // the round's sum is not the last one; it is; an earlier round's was
+struct alignas(16) verify_record {
+    int cur, a, r, kind;
+    int rej[HS_MAX_NODES], path[HS_MAX_NODES], out[HS_MAX_NODES];
+    double z[HS_MAX_NODES];
+};
+static_assert(sizeof(verify_record) <= HS_PROBS_RECORD, "the workspace's share");
 
-// Sum of one slice's weights at node cur after r rejections, by the workgroup.
+// What is left of the weights of a thread's tokens after r rejections at a node: pieces of eight tokens, the first at `from`, `step` apart.
+template <typename T>
+__device__ __forceinline__ void weights_left(const verify_args& a, int row, int from, int step, int r, const verify_left& l, double (&w)[PER]) {
+    const bool point = a.q == nullptr, draft = !point && r > 0;
+    const bool pv = whole_pieces<T>(a.p, a.p_stride), qv = whole_pieces<T>(a.q, a.q_stride);
+    const T *pr = (const T*)a.p + row * a.p_stride, *qr = (const T*)a.q + row * a.q_stride;
+    float p[PER / PIECE][PIECE], q[PER / PIECE][PIECE] = {};
+#pragma unroll
+    for (int u = 0; u < PER / PIECE; u++) {
+        load_piece(pr, from + u * step, a.vocab, pv, 0.f, p[u]);
+        if (draft) load_piece(qr, from + u * step, a.vocab, qv, 0.f, q[u]);
+    }
+#pragma unroll
+    for (int j = 0; j < PER; j++) w[j] = counted(p[j / PIECE][j % PIECE]);
+    for (int k = 0; k < r; k++) {
+        const double z = l.z[k];
+        const int rej = l.rej[k];
+#pragma unroll
+        for (int j = 0; j < PER; j++)
+            w[j] = point ? (rej == from + j / PIECE * step + j % PIECE ? 0.0 : w[j]) : fmax(w[j] - z * counted(q[j / PIECE][j % PIECE]), 0.0);
+    }
+}
+// Sum of one slice's weights, by the workgroup.
 template <typename T>
 __device__ __forceinline__ double sum_slice(const verify_args& a, int row, int slice, int r, const verify_left& l, double* red) {
-    const bool point = a.q == nullptr;
-    float p[PER], q[PER];
-    const bool pv = whole_pieces<T>(a.p, a.p_stride), qv = point || whole_pieces<T>(a.q, a.q_stride), vec = pv && qv;
-    load_tokens<T>((const T*)a.p + row * a.p_stride, a.vocab, slice, vec, p);
-    if (!point && r > 0) load_tokens<T>((const T*)a.q + row * a.q_stride, a.vocab, slice, vec, q);
-    double s = 0.0;
+    double w[PER], s = 0.0;
+    weights_left<T>(a, row, slice * SLICE + (int)threadIdx.x * PIECE, 256 * PIECE, r, l, w);
 #pragma unroll
-    for (int j = 0; j < PER; j++)
-        s += weight_left(counted(p[j]), !point && r > 0 ? counted(q[j]) : 0.0, slice_token<T>(slice, j, vec), r, l.z, l.rej, point);
+    for (int j = 0; j < PER; j++) s += w[j];
     return block_sum_f64(s, red);
 }
 
@@ -245,18 +372,28 @@ template <typename T>
 __global__ __launch_bounds__(256) void verify_sums(verify_args a, int round) {
     __shared__ verify_left left;
     __shared__ double red[4];
-    const int slice = blockIdx.x, b = blockIdx.y, lane = threadIdx.x & 63;
+    const int b = blockIdx.y, lane = threadIdx.x & 63;
     const int r0 = a.row_off[b], nn = min(a.row_off[b + 1] - r0, HS_MAX_NODES);
     if (nn <= 0) return;
     const verify_nodes n = load_nodes<T>(a, r0, nn, lane);
     const verify_walk s = walk_drafts(n, nn, a.k_stride, a.q == nullptr, round, [&](int i) {
         return sum_slices(a.sums + ((size_t)i * a.batch + b) * a.n_slices, a.n_slices, lane);
     }, lane);
+    if (blockIdx.x == 0 && threadIdx.x < 64) {
+        verify_record* rec = a.records + (size_t)round * a.batch + b;
+        if (lane == 0) *reinterpret_cast<int4*>(rec) = make_int4(s.cur, s.a, s.r, s.done ? RECORD_BEFORE : s.last ? RECORD_LAST : RECORD_MORE);
+        rec->rej[lane] = s.rej;
+        rec->path[lane] = s.path;
+        rec->out[lane] = s.out;
+        rec->z[lane] = s.z;
+    }
     if (s.done) return;
     publish(s, left, threadIdx.x);
     __syncthreads();
-    const double z = sum_slice<T>(a, r0 + s.cur, slice, s.r, left, red);
-    if (threadIdx.x == 0) a.sums[((size_t)round * a.batch + b) * a.n_slices + slice] = z;
+    for (int slice = blockIdx.x; slice < a.n_slices; slice += gridDim.x) {
+        const double z = sum_slice<T>(a, r0 + s.cur, slice, s.r, left, red);
+        if (threadIdx.x == 0) a.sums[((size_t)round * a.batch + b) * a.n_slices + slice] = z;
+    }
 }
 
 template <typename T>
@@ -267,39 +404,58 @@ __global__ __launch_bounds__(256) void verify_pick(verify_args a) {
     __shared__ double red[4], totals[HS_MAX_NODES + 2], wave_tot[4];
     __shared__ int s_first, s_last, s_pick;
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const bool point = a.q == nullptr;
+    // Everything whose place is known, at once: the records and sums of both rounds (what has not been written is not used), the number.
+    static_assert(HS_PROBS_ROUNDS == 2, "the first record or the second one");
+    const int more = a.rounds > 1 ? 1 : 0;
+    const verify_record *rec = a.records + b, *next = rec + (size_t)more * a.batch;
+    const double *sums0 = a.sums + (size_t)b * a.n_slices, *sums1 = sums0 + (size_t)more * a.batch * a.n_slices;
+    const int4 h0 = *reinterpret_cast<const int4*>(rec), h1 = *reinterpret_cast<const int4*>(next);
+    const int rej0 = rec->rej[lane], path0 = rec->path[lane], out0 = rec->out[lane];
+    const int rej1 = next->rej[lane], path1 = next->path[lane], out1 = next->out[lane];
+    const double z0 = rec->z[lane], z1 = next->z[lane];
+    const double u = (double)a.u_sample[b];
+    double part0 = lane < a.n_slices ? sums0[lane] : 0.0, part1 = lane < a.n_slices ? sums1[lane] : 0.0;
+    hs_loads_issued();
     const int r0 = a.row_off[b], nn = min(a.row_off[b + 1] - r0, HS_MAX_NODES);
     if (nn <= 0) {
         if (tid == 0) { a.accept_len[b] = 0; a.n_out[b] = 0; }
         return;
     }
-    const bool point = a.q == nullptr;
-    const verify_nodes n = load_nodes<T>(a, r0, nn, lane);
-    // (sums that the walk did not ask for have not been written: they are read, and not used)
-    for (int i = wave; i < a.rounds; i += 4) {
-        const double z = sum_slices(a.sums + ((size_t)i * a.batch + b) * a.n_slices, a.n_slices, lane);
-        if (lane == 0) totals[i] = z;
-    }
-    __syncthreads();
-    int known = a.rounds;
-    verify_walk s;
-    for (;;) {
-        s = walk_drafts(n, nn, a.k_stride, point, known, [&](int i) { return totals[i]; }, lane);
-        __syncthreads();      // (totals, left and own have been read)
+    for (int i = lane + 64; i < a.n_slices; i += 64) { part0 += sums0[i]; part1 += sums1[i]; }
+    const double total0 = wave_sum_f64(part0), total1 = wave_sum_f64(part1);
+    const bool second = more && h1.w != RECORD_BEFORE;
+    verify_walk s = {second ? h1.x : h0.x, second ? h1.y : h0.y, second ? h1.z : h0.z, second ? rej1 : rej0, second ? path1 : path0,
+                     second ? out1 : out0, second ? 1 : 0, second ? z1 : z0, false, (second ? h1.w : h0.w) == RECORD_LAST};
+    double zt = second ? total1 : total0;
+    const double* sums = second ? sums1 : sums0;
+    if (s.last && zt > 0.0) {
         publish(s, left, tid);
         __syncthreads();
-        if (s.done) break;
-        for (int i = 0; i < a.n_slices; i++) {
-            const double z = sum_slice<T>(a, r0 + s.cur, i, s.r, left, red);
-            if (tid == 0) own[i] = z;
+    } else {
+        if (tid == 0) { totals[0] = total0; totals[1] = total1; }
+        __syncthreads();
+        // more sums than there were launches for them, or nothing left: walk and sum here
+        const verify_nodes n = load_nodes<T>(a, r0, nn, lane);
+        for (int known = a.rounds;; known++) {
+            s = walk_drafts(n, nn, a.k_stride, point, known, [&](int i) { return totals[i]; }, lane);
+            __syncthreads();      // (totals, left and own have been read)
+            publish(s, left, tid);
+            __syncthreads();
+            if (s.done) break;
+            for (int i = 0; i < a.n_slices; i++) {
+                const double z = sum_slice<T>(a, r0 + s.cur, i, s.r, left, red);
+                if (tid == 0) own[i] = z;
+            }
+            __syncthreads();
+            const double z = sum_slices(own, a.n_slices, lane);
+            if (tid == 0) totals[known] = z;
+            __syncthreads();
         }
-        __syncthreads();
-        const double z = sum_slices(own, a.n_slices, lane);
-        if (tid == 0) totals[known] = z;
-        known++;
-        __syncthreads();
+        zt = totals[s.ask];
+        sums = s.ask >= a.rounds ? own : s.ask ? sums1 : sums0;
     }
-    const double* sums = s.ask < a.rounds ? a.sums + ((size_t)s.ask * a.batch + b) * a.n_slices : own;
-    const double zt = totals[s.ask], target = (double)a.u_sample[b] * zt;
+    const double target = u * zt;
     // the slice in which the running sum exceeds the target (rounding can leave it just beyond the last: that one then)
     int slice = -1, last = -1;
     double before = 0.0, upto = 0.0;
@@ -318,34 +474,35 @@ __global__ __launch_bounds__(256) void verify_pick(verify_args a) {
     if (tid == 0) { s_first = 256; s_last = -1; s_pick = -1; }
     __syncthreads();
     if (slice >= 0) {
-        const T* pr = (const T*)a.p + (size_t)(r0 + s.cur) * a.p_stride;
-        const T* qr = point ? nullptr : (const T*)a.q + (size_t)(r0 + s.cur) * a.q_stride;
-        auto left_of = [&](int i) -> double {
-            if (i >= a.vocab) return 0.0;
-            return weight_left(counted(wide(pr[i])), !point && s.r > 0 ? counted(wide(qr[i])) : 0.0, i, s.r, left.z, left.rej, point);
-        };
         // PER consecutive tokens per thread: the first thread whose running sum exceeds the target holds the token
         const int lo = slice * SLICE + tid * PER;
-        double sum = 0.0;
+        double w[PER], sum = 0.0;
+        weights_left<T>(a, r0 + s.cur, lo, PIECE, s.r, left, w);
 #pragma unroll
-        for (int j = 0; j < PER; j++) sum += left_of(lo + j);
+        for (int j = 0; j < PER; j++) sum += w[j];
         const double incl = wave_prefix_f64(sum, lane);
         if (lane == 63) wave_tot[wave] = incl;
         __syncthreads();
         double base = before + (incl - sum);
-        for (int q = 0; q < wave; q++) base += wave_tot[q];
+        for (int v = 0; v < wave; v++) base += wave_tot[v];
         if (sum > 0.0) {
             atomicMax(&s_last, tid);
             if (base + sum > target) atomicMin(&s_first, tid);
         }
         __syncthreads();
-        const int owner = s_first < 256 ? s_first : s_last;
-        if (owner >= 0 && wave == owner >> 6) {
-            const int at = slice * SLICE + owner * PER;
-            const double w = lane < PER ? left_of(at + lane) : 0.0;
-            const double cum = from_lane(base, owner & 63) + wave_prefix_f64(w, lane);
-            const unsigned long long some = __ballot(w > 0.0), hit = __ballot(w > 0.0 && cum > target);
-            if (lane == 0) s_pick = hit ? at + __ffsll(hit) - 1 : some ? at + 63 - __clzll(some) : -1;
+        // (rounding can leave the target just beyond the slice, or the thread's tokens: the last one with a weight then)
+        if (tid == (s_first < 256 ? s_first : s_last)) {
+            int pick = -1;
+            bool hit = false;
+#pragma unroll
+            for (int j = 0; j < PER; j++) {
+                base += w[j];
+                if (w[j] > 0.0 && !hit) {
+                    pick = lo + j;
+                    hit = base > target;
+                }
+            }
+            s_pick = pick;
         }
         __syncthreads();
     }
@@ -360,16 +517,37 @@ __global__ __launch_bounds__(256) void verify_pick(verify_args a) {
     }
 }
 
+// Logits that fit into the last cache are read a second time from there by a launch of their own; of more, a workgroup per row reads its row
+// twice while the cache has it, in full rounds of a row per compute unit; the rest again by two launches (1088 rows of 152064 tokens 357 -> 346 us;
+// with everything by such pairs of launches, 176 MB of logits at a time, 356).
 template <typename TI, typename TO>
-void launch_rows(const hs_ctx* ctx, const probs_args& p, hipStream_t st) {
-    const dim3 grid(std::max(1, std::min(p.rows, ctx->n_cu * 2)));
-    hipLaunchKernelGGL((probs_rows<TI, TO>), grid, dim3(1024), 0, st, p);
+void launch_rows(const hs_ctx* ctx, const probs_args& all, hipStream_t st) {
+    auto cached = [&](int rows) {
+        const size_t slices = (size_t)rows * all.n_slices;
+        return slices * PROBS_SLICE * sizeof(TI) <= HS_PROBS_CACHED && slices <= HS_PROBS_STATS;
+    };
+    probs_args p = all;
+    if (!cached(p.rows)) {
+        const int rest = p.rows % ctx->n_cu;
+        p.rows -= cached(rest) ? rest : 0;
+        if (p.rows > 0) hipLaunchKernelGGL((probs_rows<TI, TO>), dim3(std::min(p.rows, ctx->n_cu)), dim3(1024), 0, st, p);
+        p.first = p.rows;
+        p.rows = all.rows - p.first;
+        p.logits = (const TI*)p.logits + p.first * p.logits_stride;
+        p.out = (TO*)p.out + p.first * p.out_stride;
+    }
+    if (p.rows == 0) return;
+    const unsigned slices = (unsigned)p.rows * (unsigned)p.n_slices;
+    hipLaunchKernelGGL((probs_stats<TI>), dim3(slices), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((probs_write<TI, TO>), dim3(slices), dim3(256), 0, st, p);
 }
 
 template <typename T>
-void launch_verify(const verify_args& a, hipStream_t st) {
+void launch_verify(const hs_ctx* ctx, const verify_args& a, hipStream_t st) {
+    // what the device holds at once, four workgroups per compute unit: each walks once, and then sums one slice after another
+    const int per_seq = std::max(1, std::min(a.n_slices, 4 * ctx->n_cu / a.batch));
     for (int round = 0; round < a.rounds; round++)
-        hipLaunchKernelGGL((verify_sums<T>), dim3(a.n_slices, a.batch), dim3(256), 0, st, a, round);
+        hipLaunchKernelGGL((verify_sums<T>), dim3(per_seq, a.batch), dim3(256), 0, st, a, round);
     const size_t lds = (size_t)a.n_slices * sizeof(double);
     if (lds > 48 * 1024)      // (vocabularies beyond 25 million)
         (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&verify_pick<T>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -380,7 +558,7 @@ void launch_verify(const verify_args& a, hipStream_t st) {
 
 void hs_launch_probs(const hs_ctx* ctx, const hs_probs_args* args, hipStream_t st) {
     probs_args p = {args->logits, args->out, (size_t)args->logits_stride, (size_t)args->out_stride, args->live_rows, args->rows,
-                    ctx->desc.vocab, 0.f, 0.f};
+                    ctx->desc.vocab, (ctx->desc.vocab + PROBS_SLICE - 1) / PROBS_SLICE, 0, 0.f, 0.f, reinterpret_cast<float2*>(ctx->ws + ctx->lay.probs_stats)};
     const double c = std::min(1.4426950408889634 / (double)args->temperature, 1e38);      // (finite in 32 bits, too)
     p.c_hi = (float)c;
     p.c_lo = (float)(c - (double)p.c_hi);
@@ -405,7 +583,8 @@ void hs_launch_accept_probs(const hs_ctx* ctx, const hs_accept_probs_args* args,
     // (a tree of two branches forks once: the sum for its second child, and the one at the end)
     a.rounds = ctx->lim.c_max > 1 ? HS_PROBS_ROUNDS : 1;
     a.sums = reinterpret_cast<double*>(ctx->ws + ctx->lay.probs_sums);
+    a.records = reinterpret_cast<verify_record*>(ctx->ws + ctx->lay.probs_records);
     a.accept_len = step->accept_len; a.n_out = step->n_out; a.out_tok = step->out_tok; a.path_row = step->path_row;
-    if (args->type == HS_F32) launch_verify<float>(a, st);
-    else launch_verify<bf16_t>(a, st);
+    if (args->type == HS_F32) launch_verify<float>(ctx, a, st);
+    else launch_verify<bf16_t>(ctx, a, st);
 }
