@@ -214,7 +214,8 @@ __device__ __forceinline__ bool walk_keys(const win_args& a, const win_span& s, 
         for (int pp = 0; pp < 2; pp++) {
             const bf16_t* src = vp + (size_t)max(pp ? p.p1 : p.p0, 0) * page_elems;
 #pragma unroll
-            for (int dt = 0; dt < NDT; dt++) v.v[pp][dt] = *reinterpret_cast<const bf16x8*>(src + dt * 32 * 16);
+            for (int dt = 0; dt < NDT; dt++)      // (non-temporal: a line of V is one load's, a line of K several loads')
+                v.v[pp][dt] = __builtin_bit_cast(bf16x8, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + dt * 32 * 16)));
         }
     };
 
@@ -385,39 +386,27 @@ __global__ __launch_bounds__(256, 2) void window_rows(win_args a) {
     walk_partitions<HD>(a, s, bt, j, r0, nn, 4 * g + wave, 4 * a.groups, lane);
 }
 
-// Drafts of any size.  A workgroup takes a run of partitions of a (sequence, KV head) with four row tiles, a wavefront each: one stream of
-// 32-key tiles through a ring in LDS that the wavefronts fill and read together, across partitions.  The keys come from memory once for all
-// rows, and three tiles of 16 KB are on their way at any time, which loads into registers have no room for.  A tile is a page's K or V^T block
-// per wavefront, straight into LDS (the layout: sub_tile).  One barrier per tile: it says that the tile has landed (every wavefront has waited
-// for its share) and that its predecessor has been read, whose place is refilled then.  (A sequence with one row tile keeps one wavefront
-// busy with products: two workgroups per compute unit are enough for the memory's pace.)
-// There are one or two groups of four tiles (at most 256 query rows per KV head); the workgroups of the second, most of which have nothing to do,
-// come last.  (In turn with the others, live and idle workgroups alternated on the way to the shader engines, and of two places on a compute unit
-// one stayed empty: 256 sequences with a long tail of lengths, 4096 keys, 28 heads, 600 us instead of 435.)
-constexpr int WIN_RING = 4, WIN_RUN = 512;      // tiles in LDS; of a run
-constexpr int WIN_START = 3;
+// Keys k0, ... (k_end excluded) with four row tiles, a wavefront each: one stream of 32-key tiles through a ring in LDS that the wavefronts
+// fill and read together.  The keys come from memory once for all rows, and three tiles of 16 KB are on their way at any time, which loads into
+// registers have no room for.  A tile is a page's K or V^T block per wavefront, straight into LDS (the layout: sub_tile).  One barrier per
+// tile: it says that the tile has landed (every wavefront has waited for its share) and that its predecessor has been read, whose place is
+// refilled then.  idle: the wavefront has no rows, only its share of the tiles.
+// LONG: there may be more than WIN_RUN tiles (and the rows are a chunk's, whose masks are not loaded but computed).  all_lo, all_hi: see walk_keys, for this wavefront's rows.  Behind the last tile of every part_keys keys done(): the rows' state is complete,
+// and starts again.
+constexpr int WIN_RING = 4, WIN_RUN = 512;      // tiles in LDS; tiles whose pages are looked up at a time
 template <int HD>
-__global__ __launch_bounds__(256, 2) void window_rows_ring(win_args a, int tile_groups) {
+struct win_lds {
+    unsigned char ring[WIN_RING * sub_tile<HD>::BYTES];
+    int page[2 * WIN_RUN];
+};
+template <int HD, bool LONG, typename Done>
+__device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, const int32_t* __restrict__ bt, int j, int k0, int k_end,
+                                          int part_keys, int all_lo, int all_hi, row_tile<HD>& t, bool idle, win_lds<HD>& lds, Done done) {
     using T = sub_tile<HD>;
     constexpr int NKS = HD / 16, NDT = HD / 32, CPW = T::PAGE / 1024;   // 1 KB loads per wavefront and tile
     static_assert(WIN_RING == 4, "the wait counts below");
-    __shared__ __attribute__((aligned(1024))) unsigned char ring[WIN_RING * T::BYTES];
-    __shared__ int s_page[2 * WIN_RUN];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
-    const int units = a.groups * a.hkv * a.batch, unit = blockIdx.x % units, group = blockIdx.x / units;
-    const int g = unit % a.groups, pair = unit / a.groups;
-    const int j = pair % a.hkv, b = pair / a.hkv;
-    const int r0 = a.row_off[b], nn = a.row_off[b + 1] - r0;
-    const int G = a.hq / a.hkv, R = nn * G, nrt = (R + 31) >> 5;
-    const win_span s = make_span(a.seq_len[b], nn, a);
-    const int32_t* bt = a.block_table + (size_t)b * a.max_blocks;
-    const int all_lo = max(0, s.L + nn - a.window);      // (see window_rows)
-    const int c_begin = (int)((long long)s.n_parts * g / a.groups), c_end = (int)((long long)s.n_parts * (g + 1) / a.groups);
-    if (4 * group >= nrt || c_begin >= c_end) return;
-
-    // the run's tiles: n_low of them from k0 on, and then from k1 on (behind the gap between sinks and window)
-    const int p_last = s.partition(c_end - 1);
-    const int k0 = s.skip(s.partition(c_begin) * a.part_keys), k_end = min(s.total, (p_last + 1) * a.part_keys);
+    // the tiles: n_low of them from k0 on, and the others from low_to on (behind the gap between sinks and window)
     const int k1 = s.first & ~31;
     const int n_low = k0 < k1 ? (min(min(s.sink_end, k1), k_end) - k0 + 31) >> 5 : 0;
     const int low_to = k0 < k1 ? k1 : k0;
@@ -427,43 +416,54 @@ __global__ __launch_bounds__(256, 2) void window_rows_ring(win_args a, int tile_
     // the wavefront's share of a tile: K (is_v = 0) or V^T of its page `pg`
     const size_t page_bytes = (size_t)a.hkv * T::PAGE;
     const int is_v = wave & 1, pg = wave >> 1;
-    const unsigned ring_off = (unsigned)(size_t)(hs_gemm_detail::lds_ptr_t)ring + is_v * T::V + pg * T::PAGE;
+    const unsigned ring_off = (unsigned)(size_t)(hs_gemm_detail::lds_ptr_t)lds.ring + is_v * T::V + pg * T::PAGE;
     const unsigned char* base = reinterpret_cast<const unsigned char*>(is_v ? a.vc : a.kc) + (size_t)j * T::PAGE;
-    unsigned from[CPW];   // where in the page's block a lane's 16 bytes of load i come from
-#pragma unroll
-    for (int i = 0; i < CPW; i++) {
-        const int c = lane + 64 * i;
-        from[i] = is_v ? T::v_from(c) : T::k_at(c / (HD / 8), c % (HD / 8));   // (K's permutation is its own inverse)
-    }
+    // where in the page's block a lane's 16 bytes of the first load come from; those of load i lie 1 KB i further on, where K's permutation,
+    // which is its own inverse, differs by an exclusive or
+    const unsigned from = is_v ? T::v_from(lane) : T::k_at(lane / (HD / 8), lane % (HD / 8));
     const int key_row = (l32 & 16) | page_order(l32 & 15);
-
-    for (int i = tid; i < 2 * n_tiles; i += 256) {
-        const int p0 = key_of(i >> 1) + 16 * (i & 1), at = p0 >> 4;
-        int page = -1;
-        if (at < a.max_blocks && p0 < k_end && (p0 < s.sink_end || p0 + 16 > s.first)) page = bt[at];
-        s_page[i] = page < a.n_blocks ? page : -1;
-    }
-    // (one turn, but for a draft of more nodes than the launch provides for)
-    for (int tg = 4 * group; tg < nrt; tg += 4 * tile_groups) {
-        const int rt = tg + ((wave - g - j - b) & 3);      // (two of four wavefronts with rows are not the same two everywhere)
-        row_tile<HD> t;
-        load_rows<HD>(a, s, r0, nn, rt, j, all_lo, t, lane);
-        begin_tile<HD>(t);
-        // (waited for here: inside the loop the wait would be for every load in flight)
+    auto load_keys = [&](int slot, key_tile<HD>& k) __attribute__((always_inline)) {
+        int at = T::k_at(key_row, half);       // (chunk 2 ks + half: the permutation is an exclusive or, and so is 2 ks)
+        asm volatile("" : "+v"(at));
+        const unsigned char* tile = lds.ring + slot * T::BYTES;
 #pragma unroll
-        for (int ks = 0; ks < NKS; ks++) asm volatile("" : "+v"(t.qf[ks]));
-        asm volatile("" : "+v"(t.anc), "+v"(t.lo));
-        __syncthreads();      // (the pages are there, the ring has been read)
-        auto page_of = [&](int i, int pp) { return __builtin_amdgcn_readfirstlane(s_page[2 * i + pp]); };
-        int ahead = 0, f = 0, f_slot = 0, f_page = page_of(0, pg);      // ahead: tiles asked for and not yet waited for
+        for (int ks = 0; ks < NKS; ks++) k.k[ks] = *reinterpret_cast<const bf16x8*>(tile + (at ^ (ks << 5)));
+    };
+    auto scores = [&](const key_tile<HD>& k) __attribute__((always_inline)) {
+        f32x16 sc;
+#pragma unroll
+        for (int e = 0; e < 16; e++) sc[e] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ks++) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.k[ks], t.qf[ks], sc, 0, 0, 0);
+        return sc;
+    };
+    // (waited for here: inside the loop the wait would be for every load in flight)
+#pragma unroll
+    for (int ks = 0; ks < NKS; ks++) asm volatile("" : "+v"(t.qf[ks]));
+    if (!LONG) asm volatile("" : "+v"(t.anc), "+v"(t.lo));
+
+    int k_next = (k0 / part_keys + 1) * part_keys, k_first = k0;
+    bool odd = false;
+    for (int t0 = 0; t0 < n_tiles; t0 += WIN_RUN) {
+        const int t1 = LONG ? min(n_tiles, t0 + WIN_RUN) : n_tiles;
+        __syncthreads();      // (the ring and the pages have been read)
+        for (int i = tid; i < 2 * (t1 - t0); i += 256) {
+            const int p0 = key_of(t0 + (i >> 1)) + 16 * (i & 1), at = p0 >> 4;
+            int page = -1;
+            if (at < a.max_blocks && p0 < k_end && (p0 < s.sink_end || p0 + 16 > s.first)) page = bt[at];
+            lds.page[i] = page < a.n_blocks ? page : -1;
+        }
+        __syncthreads();
+        auto page_of = [&](int i, int pp) { return __builtin_amdgcn_readfirstlane(lds.page[2 * (i - t0) + pp]); };
+        int ahead = 0, f = t0, f_slot = 0, f_page = page_of(t0, pg);      // ahead: tiles asked for and not yet waited for
         auto fetch = [&]() __attribute__((always_inline)) {
             const unsigned char* src = base + (size_t)max(f_page, 0) * page_bytes;
             const unsigned dst = ring_off + f_slot * T::BYTES;
 #pragma unroll
-            for (int i = 0; i < CPW; i++) hs_gemm_detail::load_to_lds_16_stream(src, from[i], dst + i * 1024);
+            for (int i = 0; i < CPW; i++) hs_gemm_detail::load_to_lds_16_stream(src + i * 1024, is_v ? from : from ^ T::k_step(i), dst, i * 1024);
             f_slot = (f_slot + 1) & (WIN_RING - 1);
             ahead++;
-            if (++f < n_tiles) f_page = page_of(f, pg);
+            if (++f < t1) f_page = page_of(f, pg);
         };
         // waits for the wavefront's own part of the tile at the head of what it asked for, then for everybody's
         auto landed = [&](bool take_one) __attribute__((always_inline)) {
@@ -475,57 +475,41 @@ __global__ __launch_bounds__(256, 2) void window_rows_ring(win_args a, int tile_
             }
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         };
-        auto load_keys = [&](int slot, key_tile<HD>& k) __attribute__((always_inline)) {
-            int at = T::k_at(key_row, half);       // (chunk 2 ks + half: the permutation is an exclusive or, and so is 2 ks)
-            asm volatile("" : "+v"(at));
-            const unsigned char* tile = ring + slot * T::BYTES;
-#pragma unroll
-            for (int ks = 0; ks < NKS; ks++) k.k[ks] = *reinterpret_cast<const bf16x8*>(tile + (at ^ (ks << 5)));
-        };
-        auto scores = [&](const key_tile<HD>& k) __attribute__((always_inline)) {
-            f32x16 sc;
-#pragma unroll
-            for (int e = 0; e < 16; e++) sc[e] = 0.f;
-#pragma unroll
-            for (int ks = 0; ks < NKS; ks++) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.k[ks], t.qf[ks], sc, 0, 0, 0);
-            return sc;
-        };
-        while (ahead < WIN_RING - 1 && f < n_tiles) fetch();
+        while (ahead < WIN_RING - 1 && f < t1) fetch();
         landed(!is_v);      // the first keys
-        if (ahead < WIN_RING - 1 && f < n_tiles) fetch();
-        if (rt >= nrt) {
-            // (no rows: only its share of the tiles)
-            for (int i = 0; i < n_tiles; i++) {
-                landed(is_v || i + 1 < n_tiles);
-                if (ahead < WIN_RING - 1 && f < n_tiles) fetch();
+        if (ahead < WIN_RING - 1 && f < t1) fetch();
+        if (idle) {
+            for (int i = t0; i < t1; i++) {
+                landed(is_v || i + 1 < t1);
+                if (ahead < WIN_RING - 1 && f < t1) fetch();
             }
+            if (!LONG) return;
             continue;
         }
         // The keys run one tile ahead of the values, so that the next tile's first product is issued between this one's exponentials.
-        int slot = 0, c = c_begin, k_next = (s.partition(c) + 1) * a.part_keys, k_first = k0;
-        bool odd = false;
+        int slot = 0;
         f32x16 sc;
         {
             key_tile<HD> k;
             load_keys(0, k);
             sc = scores(k);
         }
-        for (int i = 0; i < n_tiles; i++) {
-            landed(is_v || i + 1 < n_tiles);      // this tile's values, the next one's keys
-            if (ahead < WIN_RING - 1 && f < n_tiles) fetch();
+        for (int i = t0; i < t1; i++) {
+            landed(is_v || i + 1 < t1);      // this tile's values, the next one's keys
+            if (ahead < WIN_RING - 1 && f < t1) fetch();
             const int kb = key_of(i), after = key_of(i + 1);
             key_tile<HD> k;
             value_tile<HD> v;
             const places here = {page_of(i, 0), page_of(i, 1)};
             load_keys((slot + 1) & (WIN_RING - 1), k);       // (of the last tile: of whatever lies there, not used)
-            const bool masked = tile_masked(a, here, kb, all_lo, s.L);
+            const bool masked = tile_masked(a, here, kb, all_lo, all_hi);
             const float alpha = take_scores<HD>(a, s, t, sc, here, masked, kb, half);
             // (only here: with the keys, the values and the masks at the same time the registers would not do)
 #pragma unroll
             for (int pp = 0; pp < 2; pp++)
 #pragma unroll
                 for (int dt = 0; dt < NDT; dt++)
-                    v.v[pp][dt] = *reinterpret_cast<const bf16x8*>(ring + slot * T::BYTES + T::V + pp * T::PAGE + dt * 1024 + T::v_at(l32, half));
+                    v.v[pp][dt] = *reinterpret_cast<const bf16x8*>(lds.ring + slot * T::BYTES + T::V + pp * T::PAGE + dt * 1024 + T::v_at(l32, half));
             if (masked) odd |= mask_values<HD>(v);
             bf16x8 pb[2];
             const f32x16 next = scores(k);
@@ -540,16 +524,51 @@ __global__ __launch_bounds__(256, 2) void window_rows_ring(win_args a, int tile_
             slot = (slot + 1) & (WIN_RING - 1);
             if (i + 1 == n_tiles || after >= k_next) {
                 if (__any(odd)) {
-                    add_odd<HD>(a, s, bt, j, k_first, min(k_end, k_next), all_lo, s.L, t, lane);
+                    add_odd<HD>(a, s, bt, j, k_first, min(k_end, k_next), all_lo, all_hi, t, lane);
                     odd = false;
                 }
-                put_partial<HD>(a, t, r0, rt, R, G, j, c, lane);
-                begin_tile<HD>(t);
-                c++;
-                k_next = (s.partition(c) + 1) * a.part_keys;
+                done();
+                k_next = (after / part_keys + 1) * part_keys;
                 k_first = after;
             }
         }
+        if (!LONG) return;
+    }
+}
+
+// Drafts of any size.  A workgroup takes a run of partitions of a (sequence, KV head) with four row tiles.  (A sequence with one row tile
+// keeps one wavefront busy with products: two workgroups per compute unit are enough for the memory's pace.)
+// There are one or two groups of four tiles (at most 256 query rows per KV head); the workgroups of the second, most of which have nothing to do,
+// come last.  (In turn with the others, live and idle workgroups alternated on the way to the shader engines, and of two places on a compute unit
+// one stayed empty: 256 sequences with a long tail of lengths, 4096 keys, 28 heads, 600 us instead of 435.)
+constexpr int WIN_START = 3;
+template <int HD>
+__global__ __launch_bounds__(256, 2) void window_rows_ring(win_args a, int tile_groups) {
+    __shared__ __attribute__((aligned(1024))) win_lds<HD> lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int units = a.groups * a.hkv * a.batch, unit = blockIdx.x % units, group = blockIdx.x / units;
+    const int g = unit % a.groups, pair = unit / a.groups;
+    const int j = pair % a.hkv, b = pair / a.hkv;
+    const int r0 = a.row_off[b], nn = a.row_off[b + 1] - r0;
+    const int G = a.hq / a.hkv, R = nn * G, nrt = (R + 31) >> 5;
+    const win_span s = make_span(a.seq_len[b], nn, a);
+    const int32_t* bt = a.block_table + (size_t)b * a.max_blocks;
+    const int all_lo = max(0, s.L + nn - a.window);      // (see walk_partitions)
+    const int c_begin = (int)((long long)s.n_parts * g / a.groups), c_end = (int)((long long)s.n_parts * (g + 1) / a.groups);
+    if (4 * group >= nrt || c_begin >= c_end) return;
+    const int k0 = s.skip(s.partition(c_begin) * a.part_keys), k_end = min(s.total, (s.partition(c_end - 1) + 1) * a.part_keys);
+    // (one turn, but for a draft of more nodes than the launch provides for)
+    for (int tg = 4 * group; tg < nrt; tg += 4 * tile_groups) {
+        const int rt = tg + ((wave - g - j - b) & 3);      // (two of four wavefronts with rows are not the same two everywhere)
+        int c = c_begin;
+        row_tile<HD> t;
+        load_rows<HD>(a, s, r0, nn, rt, j, all_lo, t, lane);
+        begin_tile<HD>(t);
+        ring_keys<HD, false>(a, s, bt, j, k0, k_end, a.part_keys, all_lo, s.L, t, rt >= nrt, lds, [&]() __attribute__((always_inline)) {
+            put_partial<HD>(a, t, r0, rt, R, G, j, c, lane);
+            begin_tile<HD>(t);
+            c++;
+        });
     }
 }
 
@@ -630,30 +649,41 @@ __global__ __launch_bounds__(256) void window_merge(win_args a) {
 }
 
 // The rows of a chunk: consecutive tokens, row i of a sequence at position L + i.  A workgroup takes 128 query rows of one (sequence, KV
-// head), a wavefront 32 of them through all their keys: with hundreds of rows per sequence there is enough to do without cutting the
-// key axis.
+// head), a wavefront 32 of them, through all their keys: with hundreds of rows per sequence there is enough to do without cutting the key axis.
+// (Every wavefront with the keys of its own 32 rows, from the caches into registers: 165 us for 8 x 512 tokens, 28 heads, 1024 keys.)
 template <int HD>
 __global__ __launch_bounds__(256, 2) void window_chunk(win_args a, int nx) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
-    const int pair = blockIdx.x / nx, j = pair % a.hkv, b = pair / a.hkv;
+    __shared__ __attribute__((aligned(1024))) win_lds<HD> lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
+    // Ids are dealt round-robin to the eight XCDs: with a multiple of eight pairs, all blocks of a pair go to one XCD and find its K and V in
+    // that L2.
+    const int pairs = a.hkv * a.batch;
+    int pair = blockIdx.x / nx, bx = blockIdx.x % nx;
+    if ((pairs & 7) == 0) {
+        const int local = blockIdx.x >> 3;
+        pair = (local / nx) * 8 + (blockIdx.x & 7);
+        bx = local % nx;
+    }
+    const int j = pair % a.hkv, b = pair / a.hkv;
     const int r0 = a.row_off[b], nn = a.row_off[b + 1] - r0;
-    const win_span s = make_span(a.seq_len[b], nn, a);
+    win_span s = make_span(a.seq_len[b], nn, a);
     if (s.n_parts == 0) return;
     const int G = a.hq / a.hkv, R = nn * G;
     const int32_t* bt = a.block_table + (size_t)b * a.max_blocks;
-    for (int rt = (blockIdx.x % nx) * 4 + wave; rt * 32 < R; rt += nx * 4) {
+    for (; bx * 128 < R; bx += nx) {
+        // the keys of the block's rows
+        s.first = max(0, s.L + bx * 128 / G + 1 - a.window);
+        s.sink_end = min(min(a.sinks, s.first), s.total);
+        const int k_end = min(s.total, s.L + min(nn - 1, (bx * 128 + 127) / G) + 1);
+        const int rt = bx * 4 + wave, rho = rt * 32 + l32;
+        const int node0 = rt * 32 / G, node1 = min(nn - 1, (rt * 32 + 31) / G), node = min(rho / G, nn - 1);
         row_tile<HD> t;
         load_query_tile<HD>(a.q, nullptr, r0, rt, R, G, a.hq, j, half, l32, t.qf, t.anc);
-        begin_tile<HD>(t);
-        const int rho = rt * 32 + l32;
-        const int node0 = rt * 32 / G, node1 = min(nn - 1, (rt * 32 + 31) / G), node = min(rho / G, nn - 1);
         t.lo = max(0, s.L + node + 1 - a.window);
         t.hi = s.L + node + 1;
-        win_span w = s;     // the keys of this tile's rows
-        w.first = max(0, s.L + node0 + 1 - a.window);
-        w.sink_end = min(min(a.sinks, w.first), s.total);
-        const int k0 = w.skip(0), k_end = min(s.total, s.L + node1 + 1), all_lo = max(0, s.L + node1 + 1 - a.window), all_hi = s.L + node0 + 1;
-        if (walk_keys<HD>(a, w, bt, j, k0, k_end, all_lo, all_hi, t, lane)) add_odd<HD>(a, w, bt, j, k0, k_end, all_lo, all_hi, t, lane);
+        begin_tile<HD>(t);
+        ring_keys<HD, true>(a, s, bt, j, s.skip(0), k_end, INT32_MAX / 2, max(0, s.L + node1 + 1 - a.window), s.L + node0 + 1, t, rt * 32 >= R, lds,
+                      [&]() __attribute__((always_inline)) {});
         if (rho >= R) continue;
         const float inv = t.l == 0.f ? 0.f : 1.f / t.l;
         bf16_t* po = a.out + ((size_t)(r0 + node) * a.hq + j * G + (rho - node * G)) * HD;
@@ -685,7 +715,7 @@ win_plan plan_rows(const hs_ctx* ctx, int window, int sinks) {
     // over the chip: a wavefront each of a draft of few rows, a workgroup each of larger ones.
     const bool wave = rows_of(ctx) <= 32;
     long long part = wave ? 1024 : 2048;
-    while (part > 64 && (long long)ctx->lim.max_batch * ctx->desc.n_kv_heads * ((span + part - 1) / part) < (wave ? 2048 : 512)) part /= 2;
+    while (part > 64 && (long long)ctx->lim.max_batch * ctx->desc.n_kv_heads * ((span + part - 1) / part) < (wave ? 1024 : 512)) part /= 2;
     while (part < ctx->att_part && most(part) > ctx->max_parts) part *= 2;      // (what the workspace holds)
     if (most(part) > ctx->max_parts) part = ctx->att_part;
     return {(int)part, (int)most(part)};
@@ -736,13 +766,12 @@ void hs_launch_window_attention(const hs_ctx* ctx, int layer, const hs_kv_cache*
         return;
     }
     // How many workgroups share the partitions of a (sequence, KV head): as many as make the fewest tiles one after the other, in
-    // rounds of two workgroups per compute unit, of which each takes as long as WIN_START tiles until its first one is there.  (Its page
-    // numbers have to fit in LDS.)
+    // rounds of two workgroups per compute unit, of which each takes as long as WIN_START tiles until its first one is there.
     const int tile_groups = (most + 127) / 128;
     long long best = 0;
     for (int groups = 1; groups <= a.max_parts; groups++) {
         const int run = (a.max_parts + groups - 1) / groups * (a.part_keys / 32);
-        if (run > WIN_RUN) continue;
+        if (run > WIN_RUN) continue;      // (one partition is at most 64 tiles)
         const long long rounds = ((long long)groups * a.hkv * a.batch + 2 * ctx->n_cu - 1) / (2 * ctx->n_cu);
         const long long cost = rounds * (WIN_START + run);
         if (a.groups == 0 || cost < best) { best = cost; a.groups = groups; }
