@@ -28,8 +28,9 @@ static inline int hs_reject_slices(int vocab) { return (vocab + HS_REJECT_SLICE 
 // Verification against probabilities: the vocabulary is summed in slices of this many tokens, for each sequence in up to
 // HS_PROBS_ROUNDS launches.
 constexpr int HS_PROBS_SLICE = 4096, HS_PROBS_ROUNDS = 2, HS_PROBS_RECORD = 1536;      // (bytes of a walk's record)
-// Softmax of logits: rows of up to so many bytes are read twice by two launches, with a maximum and a sum for each of so many slices.
-constexpr size_t HS_PROBS_CACHED = 192u << 20, HS_PROBS_STATS = 32768;
+// Softmax of logits: rows of up to so many bytes are read twice by two launches; a maximum and a sum for each of so many units of 1024 tokens
+// (a vocabulary, which hs_create keeps below 2^25, has no more).
+constexpr size_t HS_PROBS_CACHED = 192u << 20, HS_PROBS_STATS = 262144;
 static inline int hs_probs_slices(int vocab) { return (vocab + HS_PROBS_SLICE - 1) / HS_PROBS_SLICE; }
 
 struct hs_workspace_layout {

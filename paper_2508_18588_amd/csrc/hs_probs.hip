@@ -78,14 +78,17 @@ __device__ __forceinline__ bool whole_pieces(const void* p, size_t stride) {
 // ---- p[t] = exp((l[t] - max l) / T) / sum.  Bound by memory: the logits once and the probabilities once, and of the second reading of the
 // logits, when maximum and sum are known, what the caches don't have.
 
+// Maximum and sum are those of units of 1024 tokens, a wavefront each, joined in their order: a row's probabilities have the same bits whatever
+// other rows there are and however the call is launched.
+constexpr int UNIT = 1024, UNIT_PIECES = UNIT / 64 / PIECE;
 struct probs_args {
     const void* logits;
     void* out;
     size_t logits_stride, out_stride;
     const int32_t* live;      // rows that there are, or null: all
-    int rows, vocab, n_slices, first;      // first: the number of row 0 in what live counts
+    int rows, vocab, units, first;      // first: the number of row 0 in what live counts
     float c_hi, c_lo;         // log2(e) / T
-    float2* stats;            // [rows][n_slices]: largest logit and sum of a slice
+    float2* stats;            // [rows][units]: a unit's largest logit and the sum of its weights relative to that
 };
 
 // exp((l - m) / T): the exponent is a product of two parts, so that it is as exact as its result (a product rounded once is off by
@@ -96,120 +99,113 @@ __device__ __forceinline__ float weight(float l, float m, float c_hi, float c_lo
     // (an excluded logit at an infinite temperature; an exponent whose second part has lost its meaning)
     return d == -INFINITY || hi < -160.f ? 0.f : __builtin_fmaf(e * 0.6931471805599453f, lo, e);
 }
-// The sum of a thread's weights so far, relative to its largest logit, takes a piece.
-__device__ __forceinline__ void add_piece(const float (&v)[PIECE], const probs_args& p, float& m, float& s) {
-    float top = m;
-#pragma unroll
-    for (int e = 0; e < PIECE; e++) top = fmaxf(top, v[e]);
-    if (top != m) {
-        s *= weight(m, top, p.c_hi, p.c_lo);
-        m = top;
-    }
-#pragma unroll
-    for (int e = 0; e < PIECE; e++) s += v[e] == -INFINITY ? 0.f : weight(v[e], m, p.c_hi, p.c_lo);
-}
-__device__ __forceinline__ void normalise(float (&v)[PIECE], const probs_args& p, float top, float inv) {
-#pragma unroll
-    for (int e = 0; e < PIECE; e++) v[e] = (v[e] == -INFINITY ? 0.f : weight(v[e], top, p.c_hi, p.c_lo)) * inv;
-}
 __device__ __forceinline__ float wave_sum_f32(float v) {
-#pragma unroll
-    for (int k = 32; k > 0; k >>= 1) v += __shfl_xor(v, k);
+    auto step = [&](unsigned other) { v += __uint_as_float(other); };
+    step(lane_xor<32>(__float_as_uint(v)));
+    step(lane_xor<16>(__float_as_uint(v)));
+    step(lane_xor<8>(__float_as_uint(v)));
+    step(lane_xor<4>(__float_as_uint(v)));
+    step(lane_xor<2>(__float_as_uint(v)));
+    step(lane_xor<1>(__float_as_uint(v)));
     return v;
+}
+// A wavefront's unit of a row (tokens beyond the vocabulary: -inf), and what goes into the sums.
+template <typename T>
+__device__ __forceinline__ void load_unit(const T* l, int unit, int lane, const probs_args& p, bool whole, float (&v)[UNIT_PIECES][PIECE]) {
+#pragma unroll
+    for (int u = 0; u < UNIT_PIECES; u++) load_piece(l, unit * UNIT + (lane + 64 * u) * PIECE, p.vocab, whole, -INFINITY, v[u]);
+}
+__device__ __forceinline__ float2 unit_stat(const float (&v)[UNIT_PIECES][PIECE], const probs_args& p) {
+    float m = -INFINITY, s = 0.f;
+#pragma unroll
+    for (int u = 0; u < UNIT_PIECES; u++)
+#pragma unroll
+        for (int e = 0; e < PIECE; e++) m = fmaxf(m, v[u][e]);
+    m = wave_max_f32(m);
+#pragma unroll
+    for (int u = 0; u < UNIT_PIECES; u++)
+#pragma unroll
+        for (int e = 0; e < PIECE; e++) s += v[u][e] == -INFINITY ? 0.f : weight(v[u][e], m, p.c_hi, p.c_lo);
+    return make_float2(m, wave_sum_f32(s));
+}
+// The row's largest logit, and 1 / the sum of its weights, by a wavefront from the units'.
+__device__ __forceinline__ float2 join_units(const float2* stats, const probs_args& p, int lane) {
+    float m = -INFINITY, s = 0.f;
+    for (int i = lane; i < p.units; i += 64) m = fmaxf(m, stats[i].x);
+    m = wave_max_f32(m);
+    for (int i = lane; i < p.units; i += 64) {
+        const float2 x = stats[i];
+        s += x.x == -INFINITY ? x.y : x.y * weight(x.x, m, p.c_hi, p.c_lo);
+    }
+    s = wave_sum_f32(s);
+    return make_float2(m, s == 0.f ? 0.f : 1.f / s);
+}
+template <typename T>
+__device__ __forceinline__ void store_unit(T* o, int unit, int lane, const probs_args& p, bool whole, float (&v)[UNIT_PIECES][PIECE], float2 top) {
+#pragma unroll
+    for (int u = 0; u < UNIT_PIECES; u++) {
+#pragma unroll
+        for (int e = 0; e < PIECE; e++) v[u][e] = (v[u][e] == -INFINITY ? 0.f : weight(v[u][e], top.x, p.c_hi, p.c_lo)) * top.y;
+        store_piece(o, unit * UNIT + (lane + 64 * u) * PIECE, p.vocab, whole, v[u]);
+    }
 }
 
 // Many rows: a workgroup each, which takes its second pass from the row's end to its start, the last part first that the caches still have.
 // One workgroup per compute unit, so that the rows at hand (256 of 608 KB) stay in the 256 MB of the last cache.  (With 57344 tokens in registers
 // and 32768 in LDS between the passes 1088 rows took 381 us instead of 357: the caches are good enough, and the wavefronts are better off.)
+constexpr int ROW_UNITS = 4096;      // a row's units in LDS
 template <typename TI, typename TO>
 __global__ __launch_bounds__(1024) void probs_rows(probs_args p) {
-    __shared__ float red_m[16], red_s[16];
+    __shared__ float2 stats[ROW_UNITS];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int M = p.live ? min(*p.live, p.rows) : p.rows, pieces = (p.vocab + PIECE - 1) / PIECE;
+    const int M = p.live ? min(*p.live, p.rows) : p.rows;
     const bool in_whole = whole_pieces<TI>(p.logits, p.logits_stride), out_whole = whole_pieces<TO>(p.out, p.out_stride);
     for (int row = blockIdx.x; row < M; row += gridDim.x) {
         const TI* l = (const TI*)p.logits + row * p.logits_stride;
         TO* o = (TO*)p.out + row * p.out_stride;
-        float m = -INFINITY, s = 0.f;
-        for (int q = tid; q < pieces; q += 2048) {
-            float v[2][PIECE];
-#pragma unroll
-            for (int u = 0; u < 2; u++) load_piece(l, (q + 1024 * u) * PIECE, p.vocab, in_whole, -INFINITY, v[u]);
-#pragma unroll
-            for (int u = 0; u < 2; u++) add_piece(v[u], p, m, s);
-        }
-        float top = wave_max_f32(m);
         __syncthreads();      // (the row before has been read)
-        if (lane == 0) red_m[wave] = top;
-        __syncthreads();
-        top = red_m[0];
-#pragma unroll
-        for (int w = 1; w < 16; w++) top = fmaxf(top, red_m[w]);
-        s = wave_sum_f32(m == -INFINITY ? s : s * weight(m, top, p.c_hi, p.c_lo));
-        if (lane == 0) red_s[wave] = s;
-        __syncthreads();
-        float sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < 16; w++) sum += red_s[w];
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        for (int q = tid + (pieces - 1) / 2048 * 2048; q >= 0; q -= 2048) {
-            float v[2][PIECE];
-#pragma unroll
-            for (int u = 0; u < 2; u++) load_piece(l, (q + 1024 * u) * PIECE, p.vocab, in_whole, -INFINITY, v[u]);
-#pragma unroll
-            for (int u = 0; u < 2; u++) {
-                normalise(v[u], p, top, inv);
-                store_piece(o, (q + 1024 * u) * PIECE, p.vocab, out_whole, v[u]);
+        for (int k = wave; k < p.units; k += 32) {
+            float v[2][UNIT_PIECES][PIECE];
+            load_unit(l, k, lane, p, in_whole, v[0]);
+            if (k + 16 < p.units) load_unit(l, k + 16, lane, p, in_whole, v[1]);
+            float2 x = unit_stat(v[0], p);
+            if (lane == 0) stats[k] = x;
+            if (k + 16 < p.units) {
+                x = unit_stat(v[1], p);
+                if (lane == 0) stats[k + 16] = x;
             }
+        }
+        __syncthreads();
+        const float2 top = join_units(stats, p, lane);
+        for (int k = (p.units - 1) / 16 * 16 + wave; k >= 0; k -= 16) {
+            if (k >= p.units) continue;
+            float v[UNIT_PIECES][PIECE];
+            load_unit(l, k, lane, p, in_whole, v);
+            store_unit(o, k, lane, p, out_whole, v, top);
         }
     }
 }
 
-// Few rows: slices of 4096 tokens, a workgroup of 256 threads each; one launch for the slices' maxima and sums, one that joins them and writes.
-constexpr int PROBS_SLICE = 4096;
+// Few rows: a workgroup per four units; one launch for the units' maxima and sums, one that joins them and writes.
 template <typename TI>
 __global__ __launch_bounds__(256) void probs_stats(probs_args p) {
-    __shared__ float red_m[4], red_s[4];
-    const int slice = blockIdx.x % p.n_slices, row = blockIdx.x / p.n_slices, tid = threadIdx.x, wave = tid >> 6;
-    const TI* l = (const TI*)p.logits + row * p.logits_stride;
-    const bool whole = whole_pieces<TI>(p.logits, p.logits_stride);
-    float v[2][PIECE], m = -INFINITY, s = 0.f;
-    if (p.live && p.first + row >= *p.live) return;
-#pragma unroll
-    for (int u = 0; u < 2; u++) load_piece(l, slice * PROBS_SLICE + (tid + 256 * u) * PIECE, p.vocab, whole, -INFINITY, v[u]);
-#pragma unroll
-    for (int u = 0; u < 2; u++) add_piece(v[u], p, m, s);
-    const float top = block_max_f32(m, red_m);
-    s = wave_sum_f32(m == -INFINITY ? s : s * weight(m, top, p.c_hi, p.c_lo));
-    if ((tid & 63) == 0) red_s[wave] = s;
-    __syncthreads();
-    if (tid == 0) p.stats[(size_t)row * p.n_slices + slice] = make_float2(top, (red_s[0] + red_s[1]) + (red_s[2] + red_s[3]));
+    const int groups = (p.units + 3) / 4, row = blockIdx.x / groups, lane = threadIdx.x & 63;
+    const int unit = blockIdx.x % groups * 4 + (threadIdx.x >> 6);
+    if (unit >= p.units || (p.live && p.first + row >= *p.live)) return;
+    float v[UNIT_PIECES][PIECE];
+    load_unit((const TI*)p.logits + row * p.logits_stride, unit, lane, p, whole_pieces<TI>(p.logits, p.logits_stride), v);
+    const float2 x = unit_stat(v, p);
+    if (lane == 0) p.stats[(size_t)row * p.units + unit] = x;
 }
 template <typename TI, typename TO>
 __global__ __launch_bounds__(256) void probs_write(probs_args p) {
-    const int slice = blockIdx.x % p.n_slices, row = blockIdx.x / p.n_slices, tid = threadIdx.x, lane = tid & 63;
-    const TI* l = (const TI*)p.logits + row * p.logits_stride;
-    TO* o = (TO*)p.out + row * p.out_stride;
-    const bool in_whole = whole_pieces<TI>(p.logits, p.logits_stride), out_whole = whole_pieces<TO>(p.out, p.out_stride);
-    float v[2][PIECE];
-    if (p.live && p.first + row >= *p.live) return;
-#pragma unroll
-    for (int u = 0; u < 2; u++) load_piece(l, slice * PROBS_SLICE + (tid + 256 * u) * PIECE, p.vocab, in_whole, -INFINITY, v[u]);
-    const float2* stats = p.stats + (size_t)row * p.n_slices;
-    float m = -INFINITY, s = 0.f;
-    for (int i = lane; i < p.n_slices; i += 64) m = fmaxf(m, stats[i].x);
-    const float top = wave_max_f32(m);
-    for (int i = lane; i < p.n_slices; i += 64) {
-        const float2 x = stats[i];
-        s += x.x == -INFINITY ? x.y : x.y * weight(x.x, top, p.c_hi, p.c_lo);
-    }
-    s = wave_sum_f32(s);
-    const float inv = s == 0.f ? 0.f : 1.f / s;
-#pragma unroll
-    for (int u = 0; u < 2; u++) {
-        normalise(v[u], p, top, inv);
-        store_piece(o, slice * PROBS_SLICE + (tid + 256 * u) * PIECE, p.vocab, out_whole, v[u]);
-    }
+    const int groups = (p.units + 3) / 4, row = blockIdx.x / groups, lane = threadIdx.x & 63;
+    const int unit = blockIdx.x % groups * 4 + (threadIdx.x >> 6);
+    if (unit >= p.units || (p.live && p.first + row >= *p.live)) return;
+    float v[UNIT_PIECES][PIECE];
+    load_unit((const TI*)p.logits + row * p.logits_stride, unit, lane, p, whole_pieces<TI>(p.logits, p.logits_stride), v);
+    const float2 top = join_units(p.stats + (size_t)row * p.units, p, lane);
+    store_unit((TO*)p.out + row * p.out_stride, unit, lane, p, whole_pieces<TO>(p.out, p.out_stride), v, top);
 }
 
 // ---- verification.  At a node with the target's probabilities p and the draft's q: w_0 = p, Z_0 = 1; the children are tried in node
@@ -522,24 +518,31 @@ __global__ __launch_bounds__(256) void verify_pick(verify_args a) {
 // with everything by such pairs of launches, 176 MB of logits at a time, 356).
 template <typename TI, typename TO>
 void launch_rows(const hs_ctx* ctx, const probs_args& all, hipStream_t st) {
-    auto cached = [&](int rows) {
-        const size_t slices = (size_t)rows * all.n_slices;
-        return slices * PROBS_SLICE * sizeof(TI) <= HS_PROBS_CACHED && slices <= HS_PROBS_STATS;
+    auto pairs = [&](int from, int rows) {
+        for (const int per = (int)(HS_PROBS_STATS / all.units); rows > 0; from += per, rows -= per) {
+            probs_args p = all;
+            p.first = from;
+            p.rows = std::min(rows, per);
+            p.logits = (const TI*)all.logits + from * all.logits_stride;
+            p.out = (TO*)all.out + from * all.out_stride;
+            const dim3 grid((unsigned)p.rows * (unsigned)((p.units + 3) / 4));
+            hipLaunchKernelGGL((probs_stats<TI>), grid, dim3(256), 0, st, p);
+            hipLaunchKernelGGL((probs_write<TI, TO>), grid, dim3(256), 0, st, p);
+        }
     };
-    probs_args p = all;
-    if (!cached(p.rows)) {
-        const int rest = p.rows % ctx->n_cu;
-        p.rows -= cached(rest) ? rest : 0;
+    auto cached = [&](int rows) {
+        const size_t units = (size_t)rows * all.units;
+        return units * UNIT * sizeof(TI) <= HS_PROBS_CACHED && units <= HS_PROBS_STATS;
+    };
+    if (cached(all.rows) || all.units <= 16 || all.units > ROW_UNITS) {      // (a short row would leave most of a workgroup idle)
+        pairs(0, all.rows);
+    } else {
+        const int rest = cached(all.rows % ctx->n_cu) ? all.rows % ctx->n_cu : 0;
+        probs_args p = all;
+        p.rows -= rest;
         if (p.rows > 0) hipLaunchKernelGGL((probs_rows<TI, TO>), dim3(std::min(p.rows, ctx->n_cu)), dim3(1024), 0, st, p);
-        p.first = p.rows;
-        p.rows = all.rows - p.first;
-        p.logits = (const TI*)p.logits + p.first * p.logits_stride;
-        p.out = (TO*)p.out + p.first * p.out_stride;
+        pairs(p.rows, rest);
     }
-    if (p.rows == 0) return;
-    const unsigned slices = (unsigned)p.rows * (unsigned)p.n_slices;
-    hipLaunchKernelGGL((probs_stats<TI>), dim3(slices), dim3(256), 0, st, p);
-    hipLaunchKernelGGL((probs_write<TI, TO>), dim3(slices), dim3(256), 0, st, p);
 }
 
 template <typename T>
@@ -558,7 +561,7 @@ void launch_verify(const hs_ctx* ctx, const verify_args& a, hipStream_t st) {
 
 void hs_launch_probs(const hs_ctx* ctx, const hs_probs_args* args, hipStream_t st) {
     probs_args p = {args->logits, args->out, (size_t)args->logits_stride, (size_t)args->out_stride, args->live_rows, args->rows,
-                    ctx->desc.vocab, (ctx->desc.vocab + PROBS_SLICE - 1) / PROBS_SLICE, 0, 0.f, 0.f, reinterpret_cast<float2*>(ctx->ws + ctx->lay.probs_stats)};
+                    ctx->desc.vocab, (ctx->desc.vocab + UNIT - 1) / UNIT, 0, 0.f, 0.f, reinterpret_cast<float2*>(ctx->ws + ctx->lay.probs_stats)};
     const double c = std::min(1.4426950408889634 / (double)args->temperature, 1e38);      // (finite in 32 bits, too)
     p.c_hi = (float)c;
     p.c_lo = (float)(c - (double)p.c_hi);

@@ -684,13 +684,13 @@ __global__ __launch_bounds__(256, 2) void window_chunk(win_args a, int nx) {
         begin_tile<HD>(t);
         ring_keys<HD, true>(a, s, bt, j, s.skip(0), k_end, INT32_MAX / 2, max(0, s.L + node1 + 1 - a.window), s.L + node0 + 1, t, rt * 32 >= R, lds,
                       [&]() __attribute__((always_inline)) {});
-        if (rho >= R) continue;
         const float inv = t.l == 0.f ? 0.f : 1.f / t.l;
         bf16_t* po = a.out + ((size_t)(r0 + node) * a.hq + j * G + (rho - node * G)) * HD;
 #pragma unroll
         for (int dt = 0; dt < HD / 32; dt++)
 #pragma unroll
             for (int g4 = 0; g4 < 4; g4++) {
+                if (rho >= R) break;
                 u32x2 x;
                 x.x = (uint32_t)to_bf16(t.o[dt][4 * g4] * inv) | ((uint32_t)to_bf16(t.o[dt][4 * g4 + 1] * inv) << 16);
                 x.y = (uint32_t)to_bf16(t.o[dt][4 * g4 + 2] * inv) | ((uint32_t)to_bf16(t.o[dt][4 * g4 + 3] * inv) << 16);
@@ -800,7 +800,9 @@ void hs_launch_window_chunk(const hs_ctx* ctx, int layer, const hs_kv_cache* cac
                             const hs_step* step, const void* q, void* out, int chunk, int window, int sinks, hipStream_t st) {
     win_args a = make_args(ctx, layer, cache, seq, step, q, out, window, sinks);
     a.seq_len = len_plus1;
-    const int nx = (int)(((long long)chunk * (a.hq / a.hkv) + 127) / 128);
+    // (a grid has fewer than 2^24 workgroups of 256: where that is too few, they take several blocks of rows)
+    const long long most = std::max<long long>(1, (1ll << 23) / ((long long)a.hkv * a.batch));
+    const int nx = (int)std::min(most, ((long long)chunk * (a.hq / a.hkv) + 127) / 128);
     const dim3 grid((unsigned)(nx * a.hkv * a.batch));
     if (ctx->desc.head_dim == 128) hipLaunchKernelGGL((window_chunk<128>), grid, dim3(256), 0, st, a, nx);
     else hipLaunchKernelGGL((window_chunk<64>), grid, dim3(256), 0, st, a, nx);

@@ -71,6 +71,34 @@ def test_probs_for_few_and_many_rows(rows):
     eng.close()
 
 
+def test_a_rows_probabilities_do_not_depend_on_the_other_rows():
+    """The same bits whether a row is one of 330 of 600 KB, which a workgroup each takes, or of a few."""
+    vocab, rows = 151936, 330
+    eng = engine(1, 1, 64, [8] * 4, 1, vocab=vocab)
+    g = torch.Generator(device="cuda:0").manual_seed(1)
+    x = torch.randn(rows, vocab, generator=g, device="cuda:0") * 4
+    x[::7, 5000:5100] = -float("inf")
+    out, few = (torch.zeros(rows, vocab, device="cuda:0") for _ in range(2))
+    eng.probs(x, out, 0.9)
+    _check_probs(out[::40], x[::40], 0.9, torch.float32)
+    for r, n in ((0, 1), (100, 3), (200, 64), (329, 1)):
+        eng.probs(x[r:r + n], few[r:r + n], 0.9)
+        assert torch.equal(few[r:r + n], out[r:r + n])
+    eng.close()
+
+
+def test_probs_of_many_short_rows():
+    vocab, rows = 100, 300001                          # more units of a softmax than there is room for at a time
+    eng = engine(1, 1, 64, [8] * 4, 1, vocab=vocab)
+    x = torch.randn(rows, vocab, device="cuda:0")
+    out = torch.zeros(rows, vocab, device="cuda:0")
+    eng.probs(x, out, 1.0)
+    for r in (0, 262140, 300000):
+        _check_probs(out[r:r + 10], x[r:r + 10], 1.0, torch.float32)
+    assert (out.sum(-1) - 1.0).abs().max() < 1e-5
+    eng.close()
+
+
 @pytest.mark.parametrize("rows", [3, 600])
 def test_probs_of_excluded_and_odd_logits(rows):
     vocab, inf, nan = 10000, float("inf"), float("nan")
