@@ -832,7 +832,10 @@ __global__ __launch_bounds__(64) void attn_verify_plain(
         if (!vis) continue;
         if ((kp >> 4) >= max_blocks) break;
         int page = block_table[(size_t)b * max_blocks + (kp >> 4)];
-        if (page < 0 || page >= n_blocks) break;
+        if (page < 0 || page >= n_blocks) {
+            if (window > 0) continue;      // (a position without a page is not seen)
+            break;
+        }
         int ip = kp & 15;
         const T* kr = kc + layer_off + (((size_t)page * hkv + j) * 16 + ip) * hd;
         ACC dot = 0;

@@ -328,7 +328,10 @@ class Engine:
 
     def attention_window(self, layer: int, q, out, window: int, sinks: int = 0, chunk: int = 0):
         """One layer's attention with a window and sinks for the queries q [rows, n_q_heads * head_dim] of the rows laid out in
-        the step arrays (chunk = 0), or of up to `chunk` consecutive tokens per sequence (row_off alone)."""
+        the step arrays (chunk = 0), or of up to `chunk` consecutive tokens per sequence (row_off alone).  How many rows there
+        are is known on the device: q and out have at least as many."""
+        if q.shape != out.shape or q.dim() != 2 or q.shape[1] != self.shape.n_q_heads * self.shape.head_dim:
+            raise ValueError(f"queries {tuple(q.shape)}, output {tuple(out.shape)}")
         if q.dtype != out.dtype or q.dtype != (torch.float32 if self.precise else torch.bfloat16):
             raise ValueError(f"queries and output of {q.dtype}, {out.dtype}")
         if not (q.is_contiguous() and out.is_contiguous()):
@@ -347,9 +350,12 @@ class Engine:
 
     def accept_probs(self, p, q, u_accept, u_sample):
         """Acceptance of the step's drafts against the target's probabilities p [rows, vocab] and the drafts' distributions q
-        (None: they have none), with u_accept [rows] and u_sample [batch] as random numbers; commit() follows."""
+        (None: they have none), with u_accept [rows] and u_sample [batch] as random numbers; commit() follows.  How many rows
+        there are is known on the device: the arrays have at least as many."""
         if q is not None and _type(q) != _type(p):
             raise ValueError(f"probabilities of {p.dtype} and {q.dtype}")
+        if min(t.shape[1] for t in (p, q) if t is not None) < self.shape.vocab or u_sample.numel() < self.batch:
+            raise ValueError(f"probabilities {tuple(p.shape)}, {u_sample.numel()} random numbers")
         if u_accept.dtype != torch.float32 or u_sample.dtype != torch.float32 or not (u_accept.is_contiguous() and u_sample.is_contiguous()):
             raise ValueError("random numbers must be contiguous float32")
         args = hs_accept_probs_args(p.data_ptr(), None if q is None else q.data_ptr(), p.stride(0), 0 if q is None else q.stride(0),

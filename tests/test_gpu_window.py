@@ -232,6 +232,12 @@ def test_fp32_activations():
         got = run(eng, m, q, window, sinks)[:m].double()
         # products, exponentials and sums in 64 bits: the inputs' and the result's rounding, and 1e-6 for the scale in 32
         assert ((got - want).abs() <= 2.0 ** -24 * want.abs() + 2e-6 * mag + 1e-12).all(), (window, sinks)
+    eng.block_table[2, 3:9] = -1                             # positions 48 .. 143 of sequence 2
+    lost = lambda b: (np.arange(400) >= 48) & (np.arange(400) < 144) & (b == 2)
+    for window, sinks in ((30, 60), (180, 0)):
+        want, mag = reference(eng, lens, pars, q, window, sinks, blocked=lost)
+        got = run(eng, m, q, window, sinks)[:m].double()
+        assert ((got - want).abs() <= 2.0 ** -24 * want.abs() + 2e-6 * mag + 1e-12).all(), (window, sinks)
     eng.close()
 
 
@@ -325,6 +331,36 @@ def test_greedy_speculative_decoding_equals_plain_decoding_with_windows(window, 
     assert n_spec < n_plain
     full, _ = _decode(eng, prompts, none, Policy(window=8, k_fixed=0, k_max=8), 60, None, 0)
     assert any((a != b).any() for a, b in zip(plain, full))       # (the window changes what the model says)
+    eng.close()
+
+
+def test_a_recorded_step_with_windows():
+    """Decode steps replayed from a graph that was recorded with windows emit what eager steps emit; a window that is set
+    afterwards does not change the graph."""
+    from hs_inputs import make_prompts
+    from paper_2508_18588_amd.runtime import Policy
+    shape, eng = _toy(max_batch=3, k_max=4, c_max=1, max_len=200, shuffle_pages_seed=5)
+    prompts, pol = [p for p in make_prompts(3, 60, shape.vocab, seed=6)], Policy(window=8, k_fixed=4, k_max=4)
+    hists = [[np.concatenate([p[-7:], np.arange(100, 140, dtype=np.int32)])] for p in prompts]
+    want, steps = _decode(eng, prompts, hists, pol, 30, 24, 4)
+
+    def load():
+        eng.load_sequences(prompts, [30] * 3)
+        eng.set_history(hists)
+        eng.prefill(prompts)
+
+    load()
+    eng.set_rows_hint(15)
+    eng.step(pol)
+    graph = eng.capture_step(pol)
+    load()
+    eng.set_window(None)
+    for _ in range(steps):
+        graph.replay()
+        eng.poll_error()                                     # (the program synchronises in between)
+    torch.cuda.synchronize()
+    for b, t in enumerate(want):
+        assert (eng.tokens[b, :len(t)].cpu().numpy() == t).all()
     eng.close()
 
 
