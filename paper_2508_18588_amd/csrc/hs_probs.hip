@@ -398,7 +398,7 @@ __global__ __launch_bounds__(256) void verify_pick(verify_args a) {
     double* own = reinterpret_cast<double*>(dyn_lds);      // [n_slices]: sums that no launch has left
     __shared__ verify_left left;
     __shared__ double red[4], totals[HS_MAX_NODES + 2], wave_tot[4];
-    __shared__ int s_first, s_last, s_pick;
+    __shared__ int wave_first[4], wave_last[4], s_pick;
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool point = a.q == nullptr;
     // Everything whose place is known, at once: the records and sums of both rounds (what has not been written is not used), the number.
@@ -467,7 +467,7 @@ __global__ __launch_bounds__(256) void verify_pick(verify_args a) {
         upto += from_lane(incl, 63);
     }
     if (slice < 0) slice = last;
-    if (tid == 0) { s_first = 256; s_last = -1; s_pick = -1; }
+    if (tid == 0) s_pick = -1;
     __syncthreads();
     if (slice >= 0) {
         // PER consecutive tokens per thread: the first thread whose running sum exceeds the target holds the token
@@ -481,13 +481,16 @@ __global__ __launch_bounds__(256) void verify_pick(verify_args a) {
         __syncthreads();
         double base = before + (incl - sum);
         for (int v = 0; v < wave; v++) base += wave_tot[v];
-        if (sum > 0.0) {
-            atomicMax(&s_last, tid);
-            if (base + sum > target) atomicMin(&s_first, tid);
+        // (by ballots: 256 threads' atomics on one word of LDS took 4 us)
+        const unsigned long long some = __ballot(sum > 0.0), hit = __ballot(sum > 0.0 && base + sum > target);
+        if (lane == 0) {
+            wave_first[wave] = hit ? wave * 64 + __ffsll(hit) - 1 : 256;
+            wave_last[wave] = some ? wave * 64 + 63 - __clzll(some) : -1;
         }
         __syncthreads();
+        const int first = min(min(wave_first[0], wave_first[1]), min(wave_first[2], wave_first[3]));
         // (rounding can leave the target just beyond the slice, or the thread's tokens: the last one with a weight then)
-        if (tid == (s_first < 256 ? s_first : s_last)) {
+        if (tid == (first < 256 ? first : max(max(wave_last[0], wave_last[1]), max(wave_last[2], wave_last[3])))) {
             int pick = -1;
             bool hit = false;
 #pragma unroll
