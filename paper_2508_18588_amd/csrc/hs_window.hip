@@ -54,8 +54,10 @@ __device__ __forceinline__ win_span make_span(int seq_len, int nn, const win_arg
     s.sink_end = min(min(a.sinks, s.first), s.total);
     s.n_sink = (s.sink_end + a.part_keys - 1) / a.part_keys;
     s.p_first = max(s.first / a.part_keys, s.n_sink);
-    // (no more than there is room for: a draft of more nodes than the limits allow is not laid out by anybody)
-    s.n_parts = s.L < 0 || nn <= 0 ? 0 : min(a.max_parts, s.n_sink + max(0, (s.total + a.part_keys - 1) / a.part_keys - s.p_first));
+    // Each of them has a key, so that a walk over all keys comes through all of them.  (A sequence that has outgrown its table may have no
+    // key in its window.  No more than there is room for: a draft of more nodes than the limits allow is not laid out by anybody.)
+    const int n_window = s.first < s.total ? max(0, (s.total + a.part_keys - 1) / a.part_keys - s.p_first) : 0;
+    s.n_parts = s.L < 0 || nn <= 0 ? 0 : min(a.max_parts, s.n_sink + n_window);
     return s;
 }
 
@@ -667,7 +669,7 @@ __global__ __launch_bounds__(256, 2) void window_chunk(win_args a, int nx) {
     const int j = pair % a.hkv, b = pair / a.hkv;
     const int r0 = a.row_off[b], nn = a.row_off[b + 1] - r0;
     win_span s = make_span(a.seq_len[b], nn, a);
-    if (s.n_parts == 0) return;
+    if (nn <= 0) return;
     const int G = a.hq / a.hkv, R = nn * G;
     const int32_t* bt = a.block_table + (size_t)b * a.max_blocks;
     for (; bx * 128 < R; bx += nx) {

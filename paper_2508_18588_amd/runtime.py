@@ -317,6 +317,11 @@ class Engine:
 
     # ---------------------------------------------------------------- windows, probabilities
 
+    def _on_device(self, *tensors):
+        for t in tensors:
+            if t is not None and t.device != self.seq_len.device:
+                raise ValueError(f"a tensor on {t.device}, the engine is on {self.seq_len.device}")
+
     def set_window(self, window, sinks: int = 0):
         """Sliding-window attention with sinks in verify() and the prefills: one window for all layers, a list with one per
         layer (0 = none), or None to switch it off."""
@@ -336,6 +341,7 @@ class Engine:
             raise ValueError(f"queries and output of {q.dtype}, {out.dtype}")
         if not (q.is_contiguous() and out.is_contiguous()):
             raise ValueError("queries and output must be contiguous")
+        self._on_device(q, out)
         hs_attention_window(self.ctx, self.c_cache, self.c_seq, self.c_step,
                             hs_window_args(layer, window, sinks, chunk, q.data_ptr(), out.data_ptr()), self.stream())
 
@@ -344,6 +350,7 @@ class Engine:
         the step arrays hold."""
         if min(logits.shape[1], out.shape[1]) < self.shape.vocab or out.shape[0] < logits.shape[0]:
             raise ValueError(f"logits {tuple(logits.shape)}, output {tuple(out.shape)} for a vocabulary of {self.shape.vocab}")
+        self._on_device(logits, out)
         args = hs_probs_args(logits.data_ptr(), out.data_ptr(), logits.stride(0), out.stride(0), _type(logits), _type(out),
                              logits.shape[0], temperature, self.st["row_off"].data_ptr() + 4 * self.batch if live else None)
         hs_probs(self.ctx, args, self.stream())
@@ -358,6 +365,7 @@ class Engine:
             raise ValueError(f"probabilities {tuple(p.shape)}, {u_sample.numel()} random numbers")
         if u_accept.dtype != torch.float32 or u_sample.dtype != torch.float32 or not (u_accept.is_contiguous() and u_sample.is_contiguous()):
             raise ValueError("random numbers must be contiguous float32")
+        self._on_device(p, q, u_accept, u_sample)
         args = hs_accept_probs_args(p.data_ptr(), None if q is None else q.data_ptr(), p.stride(0), 0 if q is None else q.stride(0),
                                     _type(p), u_accept.data_ptr(), u_sample.data_ptr())
         hs_accept_probs(self.ctx, args, self.c_seq, self.c_step, self.stream())

@@ -437,6 +437,12 @@ def test_binding_refuses_tensors():
         eng.accept_probs(f(3, 50), f(3, 50).bfloat16(), f(3), f(1))
     with pytest.raises(ValueError):
         eng.accept_probs(f(3, 50), None, f(3).double(), f(1))
+    host = lambda *s: torch.zeros(*s)
+    for call in (lambda: eng.probs(host(3, 50), f(3, 50)), lambda: eng.probs(f(3, 50), host(3, 50)),
+                 lambda: eng.accept_probs(host(3, 50), None, f(3), f(1)), lambda: eng.accept_probs(f(3, 50), host(3, 50), f(3), f(1)),
+                 lambda: eng.accept_probs(f(3, 50), None, host(3), f(1)), lambda: eng.accept_probs(f(3, 50), None, f(3), host(1))):
+        with pytest.raises(ValueError, match="cuda"):        # memory that the device does not have
+            call()
     eng.close()
 
 

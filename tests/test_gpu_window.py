@@ -205,6 +205,33 @@ def test_rows_that_see_nothing_are_zero():
     eng.close()
 
 
+@pytest.mark.parametrize("heads", [(4, 1, 64), (8, 1, 128)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 4), (1, 70), (3, 0), (3, 2)])
+def test_a_sequence_that_has_outgrown_its_table(heads, window, sinks):
+    """Positions beyond the table are not seen: of a window that lies there nothing is left, whatever the workspace held."""
+    nodes = 5                                                # 20 or 40 query rows per KV head
+    eng = engine(*heads, [74, 60], nodes)
+    cap = eng.block_table.shape[1] * 16
+    assert cap == 96
+    table = eng.block_table[:, :6].clone()
+    for chunk in (0, nodes):
+        lens = [cap + 1, 61]                                 # sequence 0's rows lie at positions 96 .. 100
+        eng.seq_len.copy_(torch.tensor(lens, dtype=torch.int32))
+        pars = [chain(nodes - 1), chain(nodes - 1)]
+        m = lay_out_chunk(eng, [nodes, nodes]) if chunk else lay_out(eng, lens, pars)
+        q = queries(m, eng)
+        eng.workspace.fill_(0xFF)                            # (NaNs)
+        out = run(eng, m, q, window, sinks, chunk)
+        # the reference's sequence 0 has a longer table, of which nothing more is seen
+        wide = eng.block_table
+        eng.block_table = torch.cat([table, table[:, :1]], 1)
+        check(out, eng, lens, pars, q, window, sinks, chunk=bool(chunk), blocked=lambda b: np.arange(200) >= (cap if b == 0 else 200))
+        eng.block_table = wide
+        if sinks == 0:
+            assert (out[4].float() == 0).all()               # position 100: sees neither 94 nor 95
+    eng.close()
+
+
 def test_pages_behind_the_window_are_not_used():
     """Their table entries may be gone, or name a page that another sequence has."""
     lens, pars = [400, 410], [chain(3), chain(0)]
@@ -288,6 +315,9 @@ def test_binding_refuses_tensors():
             eng.attention_window(0, a, b, 4)
     with pytest.raises(ValueError):
         eng.set_window([4, 4])
+    for a, b in ((q.cpu(), q), (q, q.cpu())):                # memory that the device does not have
+        with pytest.raises(ValueError, match="cuda"):
+            eng.attention_window(0, a, b, 4)
     eng.close()
 
 
