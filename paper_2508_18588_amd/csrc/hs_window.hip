@@ -115,7 +115,10 @@ __device__ __forceinline__ bool tile_masked(const win_args& a, const places& her
     return (kb + 32 > all_hi) | ((kb < all_lo) & (kb + 32 > a.sinks)) | ((here.p0 | here.p1) < 0);
 }
 
-// Masks a tile's scores and moves the running maximum; returns what the sums so far are to be scaled by.
+// Masks a tile's scores and moves the running maximum, if they exceed it by more than WIN_LAG powers of two; returns what the sums so far are
+// to be scaled by.  What the weights are relative to need not be the maximum, only near it: weights up to 2^8 and their sums are as exact in the
+// same types, and of a tile's 32 rows nearly always some have a new maximum, few a much larger one, so that the scaling is rare.
+constexpr float WIN_LAG = 8.f;
 template <int HD>
 __device__ __forceinline__ float take_scores(const win_args& a, const win_span& s, row_tile<HD>& t, f32x16& sc,
                                              const places& here, bool masked, int kb, int half) {
@@ -133,7 +136,7 @@ __device__ __forceinline__ float take_scores(const win_args& a, const win_span& 
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(tmax), __float_as_uint(tmax), false, false);
         tmax = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.scale_log2;
     }
-    const float m_new = fmaxf(t.m, tmax);
+    const float m_new = tmax > t.m + WIN_LAG ? tmax : t.m;
     float alpha = 1.f;
     if (__any(m_new != t.m)) {
         alpha = fast_exp2(t.m - (m_new == -INFINITY ? 0.f : m_new));

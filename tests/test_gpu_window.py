@@ -88,6 +88,29 @@ def test_large_scores():
     eng.close()
 
 
+@pytest.mark.parametrize("heads", [(7, 1, 64), (8, 1, 128)])
+@pytest.mark.parametrize("rate", [0.1, 0.4, 1.0])
+def test_scores_that_rise_or_fall_along_the_keys(heads, rate):
+    """The running maximum moves all the time, a little or a lot per tile (one product per score, so that an exponent of 500 is off
+    by 2^-24 of itself for each of two roundings: 6e-5)."""
+    lens, nodes = [600, 350], 5
+    for chunk in (0, nodes):
+        eng = engine(*heads, lens, nodes, spare=nodes)
+        hq, hkv, hd = heads
+        k = eng.kc.view(torch.bfloat16).view(eng.n_layers, eng.n_blocks, hkv, 16, hd)[0]
+        k.zero_()
+        for b, n in enumerate(lens):
+            pages = eng.block_table[b, :(n + nodes) // 16 + 1].long()
+            at = torch.arange(len(pages) * 16, device="cuda:0", dtype=torch.float32).view(-1, 1, 16)
+            k[pages, :, :, 0] = (at * rate).expand(-1, hkv, -1).to(torch.bfloat16)
+        pars = [chain(nodes - 1), chain(nodes - 1)]
+        m = lay_out_chunk(eng, [nodes, nodes]) if chunk else lay_out(eng, lens, pars)
+        q = queries(m, eng)
+        for window, sinks in ((4096, 0), (200, 4)):
+            check(run(eng, m, q, window, sinks, chunk), eng, lens, pars, q, window, sinks, chunk=bool(chunk))
+        eng.close()
+
+
 def test_a_rows_result_does_not_depend_on_the_other_rows():
     """Chains decoded token by token and as one draft: the same bits (what makes greedy speculative decoding equal plain greedy
     decoding); with few and many partitions, with windows below and above the draft's length."""
