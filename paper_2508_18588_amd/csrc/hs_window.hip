@@ -515,16 +515,22 @@ __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, 
 #pragma unroll
                 for (int dt = 0; dt < NDT; dt++)
                     v.v[pp][dt] = *reinterpret_cast<const bf16x8*>(lds.ring + slot * T::BYTES + T::V + pp * T::PAGE + dt * 1024 + T::v_at(l32, half));
-            if (masked) odd |= mask_values<HD>(v);
+            if (masked) {
+                odd |= mask_values<HD>(v);
+                // (changed in place: without this the values of all tiles were copied to where the masked ones end up, 432 -> 420 us for 256
+                // drafts over 4096 keys)
+#pragma unroll
+                for (int pp = 0; pp < 2; pp++)
+#pragma unroll
+                    for (int dt = 0; dt < NDT; dt++) asm volatile("" : "+v"(v.v[pp][dt]));
+            }
             bf16x8 pb[2];
+            // (the matrix unit goes to the wavefront that has products for it, 113 -> 107 us for 8 x 512 tokens, 28 heads, 1024 keys)
+            __builtin_amdgcn_s_setprio(1);
             const f32x16 next = scores(k);
             take_probabilities<HD>(a, t, sc, alpha, pb);
             take_values<HD>(t, v, pb);
-#pragma unroll
-            for (int q = 0; q < NKS; q++) {             // a product, its share of the exponentials
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x402, 64 / NKS, 0);
-            }
+            __builtin_amdgcn_s_setprio(0);
             sc = next;
             slot = (slot + 1) & (WIN_RING - 1);
             if (i + 1 == n_tiles || after >= k_next) {
