@@ -7,12 +7,18 @@
 // A sequence of L cached tokens and nn rows needs the keys [0, sinks) and [L + 1 - window, L + nn), whatever its length: only
 // their pages are looked up and read.
 //
-// One wavefront takes a tile of 32 query rows (rows of one token's G query heads, which share a KV head, are neighbours) through
-// a run of keys, 32 at a time, without the LDS: the matrix instructions' operands are loaded from the cache as they are needed.
-// Scores are computed transposed, S^T = K . Q^T (v_mfma_f32_32x32x16_bf16), so that a lane has the scores of one query row and the
-// softmax statistics are its own scalars.  The second product O^T = V^T . P^T takes 16 tokens of V^T, which the cache holds token
-// index fastest: a lane's operand is 16 contiguous bytes, tokens 8 half .. 8 half + 7 of a page.  The rows of the first product's
-// operand are therefore the page's keys in the order of page_order, which leaves a lane exactly the probabilities of those tokens.
+// Scores are computed transposed, S^T = K . Q^T (v_mfma_f32_32x32x16_bf16), for 32 query rows (rows of one token's G query heads, which share a
+// KV head, are neighbours) and 32 keys at a time, so that a lane has the scores of one query row and the softmax statistics are its own scalars.
+// The second product O^T = V^T . P^T takes 16 tokens of V^T, which the cache holds token index fastest: a lane's operand is 16 contiguous bytes,
+// tokens 8 half .. 8 half + 7 of a page.  The rows of the first product's operand are therefore the page's keys in the order of page_order, which
+// leaves a lane exactly the probabilities of those tokens.
+//
+// A draft's rows are few and its keys many: memory bounds it, and the keys are cut into partitions, whose results are joined by a launch of
+// their own.  Up to 32 query rows per KV head (plain decoding): a wavefront per partition, operands straight from the cache into registers
+// (128 sequences, 28 heads, 1024 keys: 58 us, 4.65 TB/s; a copy reaches 4.9).  More: four row tiles share a stream of key tiles through LDS (256
+// drafts, 4096 keys: 417 us, 4.5 TB/s; 64 trees of 17 nodes, 40 heads, 2048 keys: 132 us, 4.3 TB/s).  A chunk's rows are many: a workgroup takes 128
+// of them through all their keys (8 x 512 tokens, 28 heads, 1024 keys: 104 us, 580 TFLOP/s of the 1215 that a large product of matrices
+// reaches; matrix unit, vector unit and LDS are each busy for two fifths of the time, with two wavefronts per SIMD to overlap them).
 //
 // Every sum has an order that depends on absolute key positions only (32-key tiles, partitions of part_keys, merged in index order;
 // keys that a row does not see contribute exact zeros): a row's result does not depend on what other rows are computed with it.
@@ -396,13 +402,13 @@ __global__ __launch_bounds__(256, 2) void window_rows(win_args a) {
 // registers have no room for.  A tile is a page's K or V^T block per wavefront, straight into LDS (the layout: sub_tile).  One barrier per
 // tile: it says that the tile has landed (every wavefront has waited for its share) and that its predecessor has been read, whose place is
 // refilled then.  idle: the wavefront has no rows, only its share of the tiles.
-// LONG: there may be more than WIN_RUN tiles (and the rows are a chunk's, whose masks are not loaded but computed).  all_lo, all_hi: see walk_keys, for this wavefront's rows.  Behind the last tile of every part_keys keys done(): the rows' state is complete,
-// and starts again.
+// LONG: there may be more than WIN_RUN tiles (and the rows are a chunk's, whose masks are not loaded but computed).  all_lo, all_hi: see
+// walk_keys, for this wavefront's rows.  Behind the last tile of every part_keys keys done(): the rows' state is complete, and starts again.
 constexpr int WIN_RING = 4, WIN_RUN = 512;      // tiles in LDS; tiles whose pages are looked up at a time
 template <int HD>
 struct win_lds {
     unsigned char ring[WIN_RING * sub_tile<HD>::BYTES];
-    int page[2 * WIN_RUN];
+    int page[2 * WIN_RUN + 2];      // (a tile more is looked at than there are)
 };
 template <int HD, bool LONG, typename Done>
 __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, const int32_t* __restrict__ bt, int j, int k0, int k_end,
@@ -459,16 +465,17 @@ __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, 
             lds.page[i] = page < a.n_blocks ? page : -1;
         }
         __syncthreads();
-        auto page_of = [&](int i, int pp) { return __builtin_amdgcn_readfirstlane(lds.page[2 * (i - t0) + pp]); };
-        int ahead = 0, f = t0, f_slot = 0, f_page = page_of(t0, pg);      // ahead: tiles asked for and not yet waited for
+        // (read long before they are used, which is when they go to a scalar register: a trip to the LDS takes longer than the rest of a fetch)
+        auto pages_of = [&](int i) __attribute__((always_inline)) { return *reinterpret_cast<const int2*>(&lds.page[2 * (i - t0)]); };
+        int ahead = 0, f = t0, f_slot = 0, f_page = lds.page[pg];      // ahead: tiles asked for and not yet waited for
         auto fetch = [&]() __attribute__((always_inline)) {
-            const unsigned char* src = base + (size_t)max(f_page, 0) * page_bytes;
+            const unsigned char* src = base + (size_t)max(__builtin_amdgcn_readfirstlane(f_page), 0) * page_bytes;
             const unsigned dst = ring_off + f_slot * T::BYTES;
 #pragma unroll
             for (int i = 0; i < CPW; i++) hs_gemm_detail::load_to_lds_16_stream(src + i * 1024, is_v ? from : from ^ T::k_step(i), dst, i * 1024);
             f_slot = (f_slot + 1) & (WIN_RING - 1);
             ahead++;
-            if (++f < t1) f_page = page_of(f, pg);
+            if (++f < t1) f_page = lds.page[2 * (f - t0) + pg];
         };
         // waits for the wavefront's own part of the tile at the head of what it asked for, then for everybody's
         auto landed = [&](bool take_one) __attribute__((always_inline)) {
@@ -491,9 +498,10 @@ __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, 
             if (!LONG) return;
             continue;
         }
-        // The keys run one tile ahead of the values, so that the next tile's first product is issued between this one's exponentials.
+        // The keys run one tile ahead of the values: the next tile's first product needs nothing of this one's exponentials.
         int slot = 0;
         f32x16 sc;
+        int2 pages = pages_of(t0);
         {
             key_tile<HD> k;
             load_keys(0, k);
@@ -505,7 +513,8 @@ __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, 
             const int kb = key_of(i), after = key_of(i + 1);
             key_tile<HD> k;
             value_tile<HD> v;
-            const places here = {page_of(i, 0), page_of(i, 1)};
+            const places here = {__builtin_amdgcn_readfirstlane(pages.x), __builtin_amdgcn_readfirstlane(pages.y)};
+            pages = pages_of(i + 1);
             load_keys((slot + 1) & (WIN_RING - 1), k);       // (of the last tile: of whatever lies there, not used)
             const bool masked = tile_masked(a, here, kb, all_lo, all_hi);
             const float alpha = take_scores<HD>(a, s, t, sc, here, masked, kb, half);
