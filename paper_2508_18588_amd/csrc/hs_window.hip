@@ -121,11 +121,13 @@ __device__ __forceinline__ bool tile_masked(const win_args& a, const places& her
     return (kb + 32 > all_hi) | ((kb < all_lo) & (kb + 32 > a.sinks)) | ((here.p0 | here.p1) < 0);
 }
 
-// Masks a tile's scores and moves the running maximum, if they exceed it by more than WIN_LAG powers of two; returns what the sums so far are
-// to be scaled by.  What the weights are relative to need not be the maximum, only near it: weights up to 2^8 and their sums are as exact in the
-// same types, and of a tile's 32 rows nearly always some have a new maximum, few a much larger one, so that the scaling is rare.
-constexpr float WIN_LAG = 8.f;
-template <int HD>
+// Masks a tile's scores and moves the running maximum, if they exceed it by more than LAG powers of two; returns what the sums so far are to be
+// scaled by.  What the weights are relative to need not be the maximum, only near it: of a tile's 32 rows nearly always some have a new maximum,
+// few a much larger one, so that with a lag of 8 the scaling, 64 products per tile, is rare (8 x 512 tokens 123 -> 113 us, 256 drafts 445 -> 432).
+// Weights up to 2^8 and their sums are as exact in the same types, but the largest is not exactly 1 any more and is rounded as the others are:
+// the error against 64 bits grows from 0.0020 to 0.0023 of the result, of which its own rounding to bf16 is 0.0017.  Where registers are
+// loaded from memory and memory sets the pace (window_rows), there is no lag.
+template <int HD, int LAG>
 __device__ __forceinline__ float take_scores(const win_args& a, const win_span& s, row_tile<HD>& t, f32x16& sc,
                                              const places& here, bool masked, int kb, int half) {
     constexpr int NDT = HD / 32;
@@ -142,7 +144,7 @@ __device__ __forceinline__ float take_scores(const win_args& a, const win_span& 
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(tmax), __float_as_uint(tmax), false, false);
         tmax = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.scale_log2;
     }
-    const float m_new = tmax > t.m + WIN_LAG ? tmax : t.m;
+    const float m_new = LAG ? (tmax > t.m + (float)LAG ? tmax : t.m) : fmaxf(t.m, tmax);
     float alpha = 1.f;
     if (__any(m_new != t.m)) {
         alpha = fast_exp2(t.m - (m_new == -INFINITY ? 0.f : m_new));
@@ -252,7 +254,7 @@ __device__ __forceinline__ bool walk_keys(const win_args& a, const win_span& s, 
         }
         bf16x8 pb[2];
         const bool masked = tile_masked(a, here, kb, all_lo, all_hi);
-        const float alpha = take_scores<HD>(a, s, t, sc, here, masked, kb, half);
+        const float alpha = take_scores<HD, 0>(a, s, t, sc, here, masked, kb, half);
         take_probabilities<HD>(a, t, sc, alpha, pb);
         if (masked) odd |= mask_values<HD>(v);
         take_values<HD>(t, v, pb);
@@ -517,7 +519,7 @@ __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, 
             pages = pages_of(i + 1);
             load_keys((slot + 1) & (WIN_RING - 1), k);       // (of the last tile: of whatever lies there, not used)
             const bool masked = tile_masked(a, here, kb, all_lo, all_hi);
-            const float alpha = take_scores<HD>(a, s, t, sc, here, masked, kb, half);
+            const float alpha = take_scores<HD, 8>(a, s, t, sc, here, masked, kb, half);
             // (only here: with the keys, the values and the masks at the same time the registers would not do)
 #pragma unroll
             for (int pp = 0; pp < 2; pp++)
