@@ -13,14 +13,14 @@
 // tokens 8 half .. 8 half + 7 of a page.  The rows of the first product's operand are therefore the page's keys in the order of page_order, which
 // leaves a lane exactly the probabilities of those tokens.
 //
-// A draft's rows are few and its keys many: memory bounds it, and the keys are cut into partitions, whose results are joined by a launch of
-// their own.  Up to 32 query rows per KV head (plain decoding): a wavefront per partition, operands straight from the cache into registers
-// (128 sequences, 28 heads, 1024 keys: 58 us, 4.65 TB/s; a copy reaches 4.9).  More: four row tiles share a stream of key tiles through LDS (256
-// drafts, 4096 keys: 417 us, 4.5 TB/s; 64 trees of 17 nodes, 40 heads, 2048 keys: 132 us, 4.3 TB/s).  A chunk's rows are many: a workgroup takes 128
-// of them through all their keys (8 x 512 tokens, 28 heads, 1024 keys: 104 us, 580 TFLOP/s of the 1215 that a large product of matrices
-// reaches; matrix unit, vector unit and LDS are each busy for two fifths of the time, with two wavefronts per SIMD to overlap them).
+// A draft's rows are few and its keys many, and memory bounds it.  Four row tiles share a stream of key tiles through LDS; a workgroup walks all
+// keys of a (sequence, KV head), or a run of partitions, whose results a launch of its own joins (see plan_rows).  128 single tokens, 28 heads,
+// 1024 keys: 54 us, 5.0 TB/s (a copy reaches 4.9); 256 drafts, 4096 keys: 365 us, 5.1 TB/s; 64 trees of 17 nodes, 40 heads, 2048 keys: 101 us, 5.6
+// TB/s; the stream alone, without products, 319 and 95 us.  A chunk's rows are many: a workgroup takes 128 of them through all their keys (8 x
+// 512 tokens, 28 heads, 1024 keys: 100 us, 600 TFLOP/s of the 1215 that a large product of matrices reaches; matrix unit, vector unit and LDS are
+// each busy for two fifths of the time, with two wavefronts per SIMD to overlap them).
 //
-// Every sum has an order that depends on absolute key positions only (32-key tiles, partitions of part_keys, merged in index order;
+// Every sum has an order that depends on absolute key positions only (32-key tiles, partitions of part_keys, if any, merged in index order;
 // keys that a row does not see contribute exact zeros): a row's result does not depend on what other rows are computed with it.
 #include <algorithm>
 
@@ -39,8 +39,9 @@ struct win_args {
     bf16_t* out;
     _Float16* part_o;
     float* part_ml;
-    int batch, max_blocks, n_blocks, hq, hkv, window, sinks, part_keys, max_parts, groups;
-    float scale_log2;
+    int batch, max_blocks, n_blocks, hq, hkv, window, sinks, part_keys, max_parts, groups, kind;
+    size_t part_rows;                   // rows of partial results of a partition: those of the limits' rows and all heads
+    float scale_log2, lag;
 };
 
 // The keys that a sequence's rows need: [0, sink_end) and [first, total), and the partitions of the key axis that hold them: n_sink
@@ -121,13 +122,13 @@ __device__ __forceinline__ bool tile_masked(const win_args& a, const places& her
     return (kb + 32 > all_hi) | ((kb < all_lo) & (kb + 32 > a.sinks)) | ((here.p0 | here.p1) < 0);
 }
 
-// Masks a tile's scores and moves the running maximum, if they exceed it by more than LAG powers of two; returns what the sums so far are to be
-// scaled by.  What the weights are relative to need not be the maximum, only near it: of a tile's 32 rows nearly always some have a new maximum,
-// few a much larger one, so that with a lag of 8 the scaling, 64 products per tile, is rare (8 x 512 tokens 123 -> 113 us, 256 drafts 445 -> 432).
-// Weights up to 2^8 and their sums are as exact in the same types, but the largest is not exactly 1 any more and is rounded as the others are:
-// the error against 64 bits grows from 0.0020 to 0.0023 of the result, of which its own rounding to bf16 is 0.0017.  Where registers are
-// loaded from memory and memory sets the pace (window_rows), there is no lag.
-template <int HD, int LAG>
+// Masks a tile's scores and moves the running maximum, if they exceed it by more than `lag` powers of two; returns what the sums so far are to
+// be scaled by.  What the weights are relative to need not be the maximum, only near it: of a tile's 32 rows nearly always some have a new
+// maximum, few a much larger one, so that with a lag of 8 the scaling, 64 products per tile, is rare (8 x 512 tokens 123 -> 113 us, 256 drafts
+// 445 -> 432).  Weights up to 2^8 and their sums are as exact in the same types, but the largest is not exactly 1 any more and is rounded as the
+// others are: the error against 64 bits grows from 0.0020 to 0.0023 of the result, of which its own rounding to bf16 is 0.0017.  Where one
+// wavefront of four has rows (at most 32 per KV head) memory sets the pace, and there is no lag.
+template <int HD>
 __device__ __forceinline__ float take_scores(const win_args& a, const win_span& s, row_tile<HD>& t, f32x16& sc,
                                              const places& here, bool masked, int kb, int half) {
     constexpr int NDT = HD / 32;
@@ -144,7 +145,7 @@ __device__ __forceinline__ float take_scores(const win_args& a, const win_span& 
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(tmax), __float_as_uint(tmax), false, false);
         tmax = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.scale_log2;
     }
-    const float m_new = LAG ? (tmax > t.m + (float)LAG ? tmax : t.m) : fmaxf(t.m, tmax);
+    const float m_new = tmax > t.m + a.lag ? tmax : t.m;
     float alpha = 1.f;
     if (__any(m_new != t.m)) {
         alpha = fast_exp2(t.m - (m_new == -INFINITY ? 0.f : m_new));
@@ -254,7 +255,7 @@ __device__ __forceinline__ bool walk_keys(const win_args& a, const win_span& s, 
         }
         bf16x8 pb[2];
         const bool masked = tile_masked(a, here, kb, all_lo, all_hi);
-        const float alpha = take_scores<HD, 0>(a, s, t, sc, here, masked, kb, half);
+        const float alpha = take_scores<HD>(a, s, t, sc, here, masked, kb, half);
         take_probabilities<HD>(a, t, sc, alpha, pb);
         if (masked) odd |= mask_values<HD>(v);
         take_values<HD>(t, v, pb);
@@ -315,7 +316,7 @@ __device__ __forceinline__ void put_partial(const win_args& a, const row_tile<HD
     const int half = lane >> 5, rho = rt * 32 + (lane & 31);
     const float inv = t.l > 0.f ? 1.f / t.l : 0.f;      // a partition in which the row sees no key: all zero
     const int node = rho / G;
-    const size_t prow = ((size_t)(r0 + node) * a.hq + j * G + (rho - node * G)) * a.max_parts + c;
+    const size_t prow = c * a.part_rows + (size_t)(r0 + node) * a.hq + j * G + (rho - node * G);
     _Float16* po = a.part_o + prow * HD + 8 * half;
 #pragma unroll
     for (int dt = 0; dt < HD / 32; dt++)
@@ -333,6 +334,24 @@ __device__ __forceinline__ void put_partial(const win_args& a, const row_tile<HD
             if (rho < R) *reinterpret_cast<u32x4*>(po + dt * 32 + 8 * g) = u32x4{lo[0], hi[0], lo[1], hi[1]};
         }
     if (half == 0 && rho < R) *reinterpret_cast<float2*>(a.part_ml + 2 * prow) = make_float2(t.m, t.l);
+}
+
+// The result of the lane's row.
+template <int HD>
+__device__ __forceinline__ void put_result(const win_args& a, const row_tile<HD>& t, int r0, int rt, int R, int G, int j, int lane) {
+    const int half = lane >> 5, rho = rt * 32 + (lane & 31), node = rho / G;
+    const float inv = t.l == 0.f ? 0.f : 1.f / t.l;
+    bf16_t* po = a.out + ((size_t)(r0 + node) * a.hq + j * G + (rho - node * G)) * HD;
+#pragma unroll
+    for (int dt = 0; dt < HD / 32; dt++)
+#pragma unroll
+        for (int g4 = 0; g4 < 4; g4++) {
+            if (rho >= R) break;
+            u32x2 x;
+            x.x = (uint32_t)to_bf16(t.o[dt][4 * g4] * inv) | ((uint32_t)to_bf16(t.o[dt][4 * g4 + 1] * inv) << 16);
+            x.y = (uint32_t)to_bf16(t.o[dt][4 * g4 + 2] * inv) | ((uint32_t)to_bf16(t.o[dt][4 * g4 + 3] * inv) << 16);
+            *reinterpret_cast<u32x2*>(po + dt * 32 + 8 * g4 + 4 * half) = x;
+        }
 }
 
 // A draft's row tile before its first key.
@@ -386,7 +405,7 @@ __device__ __forceinline__ void walk_partitions(const win_args& a, const win_spa
         }
 }
 
-// Drafts of at most 32 query rows per KV head (plain decoding, as a rule): a wavefront per partition.
+// Small calls of at most 32 query rows per KV head (plain decoding): a wavefront per partition.
 template <int HD>
 __global__ __launch_bounds__(256, 2) void window_rows(win_args a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
@@ -412,6 +431,15 @@ struct win_lds {
     unsigned char ring[WIN_RING * sub_tile<HD>::BYTES];
     int page[2 * WIN_RUN + 2];      // (a tile more is looked at than there are)
 };
+// Two pieces of a page's block, 1 KB apart in memory and in LDS, as load_to_lds_16_stream loads one: an instruction's constant offset counts for
+// both addresses.
+__device__ __forceinline__ __attribute__((always_inline)) void load_pair(const unsigned char* base, unsigned off0, unsigned off1, unsigned lds_off,
+                                                                         const int add) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3 offset:%4 nt\n\tglobal_load_lds_dwordx4 %2, %3 offset:%5 nt"
+                 :
+                 : "s"(lds_off), "v"(off0), "v"(off1), "s"(base), "i"(add), "i"(add + 1024)
+                 : "memory", "m0");
+}
 template <int HD, bool LONG, typename Done>
 __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, const int32_t* __restrict__ bt, int j, int k0, int k_end,
                                           int part_keys, int all_lo, int all_hi, row_tile<HD>& t, bool idle, win_lds<HD>& lds, Done done) {
@@ -427,7 +455,7 @@ __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, 
     auto key_of = [&](int i) { return i < n_low ? k0 + 32 * i : low_to + 32 * (i - n_low); };
 
     // the wavefront's share of a tile: K (is_v = 0) or V^T of its page `pg`
-    const size_t page_bytes = (size_t)a.hkv * T::PAGE;
+    const unsigned page_bytes = (unsigned)a.hkv * T::PAGE;
     const int is_v = wave & 1, pg = wave >> 1;
     const unsigned ring_off = (unsigned)(size_t)(hs_gemm_detail::lds_ptr_t)lds.ring + is_v * T::V + pg * T::PAGE;
     const unsigned char* base = reinterpret_cast<const unsigned char*>(is_v ? a.vc : a.kc) + (size_t)j * T::PAGE;
@@ -455,8 +483,7 @@ __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, 
     for (int ks = 0; ks < NKS; ks++) asm volatile("" : "+v"(t.qf[ks]));
     if (!LONG) asm volatile("" : "+v"(t.anc), "+v"(t.lo));
 
-    int k_next = (k0 / part_keys + 1) * part_keys, k_first = k0;
-    bool odd = false;
+    int k_next = (k0 / part_keys + 1) * part_keys, k_first = k0, odd = 0;
     for (int t0 = 0; t0 < n_tiles; t0 += WIN_RUN) {
         const int t1 = LONG ? min(n_tiles, t0 + WIN_RUN) : n_tiles;
         __syncthreads();      // (the ring and the pages have been read)
@@ -474,19 +501,17 @@ __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, 
             const unsigned char* src = base + (size_t)max(__builtin_amdgcn_readfirstlane(f_page), 0) * page_bytes;
             const unsigned dst = ring_off + f_slot * T::BYTES;
 #pragma unroll
-            for (int i = 0; i < CPW; i++) hs_gemm_detail::load_to_lds_16_stream(src + i * 1024, is_v ? from : from ^ T::k_step(i), dst, i * 1024);
+            for (int i = 0; i < CPW; i += 2) load_pair(src, is_v ? from : from ^ T::k_step(i), is_v ? from : from ^ T::k_step(i + 1), dst, i * 1024);
             f_slot = (f_slot + 1) & (WIN_RING - 1);
             ahead++;
             if (++f < t1) f_page = lds.page[2 * (f - t0) + pg];
         };
         // waits for the wavefront's own part of the tile at the head of what it asked for, then for everybody's
         auto landed = [&](bool take_one) __attribute__((always_inline)) {
-            if (take_one) {
-                ahead--;
-                if (ahead >= 2) HS_WAIT_VMCNT(2 * CPW);
-                else if (ahead == 1) HS_WAIT_VMCNT(CPW);
-                else HS_WAIT_VMCNT(0);
-            }
+            // (as long as there are tiles to ask for, three are on their way)
+            if (f < t1) HS_WAIT_VMCNT(2 * CPW);
+            else HS_WAIT_VMCNT(0);
+            if (take_one) ahead--;
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         };
         while (ahead < WIN_RING - 1 && f < t1) fetch();
@@ -509,17 +534,17 @@ __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, 
             load_keys(0, k);
             sc = scores(k);
         }
-        for (int i = t0; i < t1; i++) {
+        for (int i = t0, kb = key_of(t0), after; i < t1; i++, kb = after) {
             landed(is_v || i + 1 < t1);      // this tile's values, the next one's keys
             if (ahead < WIN_RING - 1 && f < t1) fetch();
-            const int kb = key_of(i), after = key_of(i + 1);
+            after = i + 1 == n_low ? low_to : kb + 32;
             key_tile<HD> k;
             value_tile<HD> v;
             const places here = {__builtin_amdgcn_readfirstlane(pages.x), __builtin_amdgcn_readfirstlane(pages.y)};
             pages = pages_of(i + 1);
             load_keys((slot + 1) & (WIN_RING - 1), k);       // (of the last tile: of whatever lies there, not used)
             const bool masked = tile_masked(a, here, kb, all_lo, all_hi);
-            const float alpha = take_scores<HD, 8>(a, s, t, sc, here, masked, kb, half);
+            const float alpha = take_scores<HD>(a, s, t, sc, here, masked, kb, half);
             // (only here: with the keys, the values and the masks at the same time the registers would not do)
 #pragma unroll
             for (int pp = 0; pp < 2; pp++)
@@ -527,7 +552,7 @@ __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, 
                 for (int dt = 0; dt < NDT; dt++)
                     v.v[pp][dt] = *reinterpret_cast<const bf16x8*>(lds.ring + slot * T::BYTES + T::V + pp * T::PAGE + dt * 1024 + T::v_at(l32, half));
             if (masked) {
-                odd |= mask_values<HD>(v);
+                odd |= __any(mask_values<HD>(v));
                 // (changed in place: without this the values of all tiles were copied to where the masked ones end up, 432 -> 420 us for 256
                 // drafts over 4096 keys)
 #pragma unroll
@@ -545,9 +570,9 @@ __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, 
             sc = next;
             slot = (slot + 1) & (WIN_RING - 1);
             if (i + 1 == n_tiles || after >= k_next) {
-                if (__any(odd)) {
+                if (odd) {
                     add_odd<HD>(a, s, bt, j, k_first, min(k_end, k_next), all_lo, all_hi, t, lane);
-                    odd = false;
+                    odd = 0;
                 }
                 done();
                 k_next = (after / part_keys + 1) * part_keys;
@@ -558,13 +583,13 @@ __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, 
     }
 }
 
-// Drafts of any size.  A workgroup takes a run of partitions of a (sequence, KV head) with four row tiles.  (A sequence with one row tile
-// keeps one wavefront busy with products: two workgroups per compute unit are enough for the memory's pace.)
+// Drafts of any size.  A workgroup takes all keys (WHOLE) or a run of partitions of a (sequence, KV head) with four row tiles.  (A sequence with
+// one row tile keeps one wavefront busy with products: two workgroups per compute unit are enough for the memory's pace.)
 // There are one or two groups of four tiles (at most 256 query rows per KV head); the workgroups of the second, most of which have nothing to do,
 // come last.  (In turn with the others, live and idle workgroups alternated on the way to the shader engines, and of two places on a compute unit
 // one stayed empty: 256 sequences with a long tail of lengths, 4096 keys, 28 heads, 600 us instead of 435.)
 constexpr int WIN_START = 3;
-template <int HD>
+template <int HD, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void window_rows_ring(win_args a, int tile_groups) {
     __shared__ __attribute__((aligned(1024))) win_lds<HD> lds;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -577,8 +602,10 @@ __global__ __launch_bounds__(256, 2) void window_rows_ring(win_args a, int tile_
     const int32_t* bt = a.block_table + (size_t)b * a.max_blocks;
     const int all_lo = max(0, s.L + nn - a.window);      // (see walk_partitions)
     const int c_begin = (int)((long long)s.n_parts * g / a.groups), c_end = (int)((long long)s.n_parts * (g + 1) / a.groups);
-    if (4 * group >= nrt || c_begin >= c_end) return;
-    const int k0 = s.skip(s.partition(c_begin) * a.part_keys), k_end = min(s.total, (s.partition(c_end - 1) + 1) * a.part_keys);
+    if (4 * group >= nrt || (!WHOLE && c_begin >= c_end)) return;
+    const int k0 = s.skip(WHOLE ? 0 : s.partition(c_begin) * a.part_keys);
+    const int k_end = !WHOLE ? min(s.total, (s.partition(c_end - 1) + 1) * a.part_keys)
+                             : s.n_parts > 0 ? min(s.total, s.L + HS_MAX_NODES) : 0;      // (no row sees a slot beyond those of 64 nodes)
     // (one turn, but for a draft of more nodes than the launch provides for)
     for (int tg = 4 * group; tg < nrt; tg += 4 * tile_groups) {
         const int rt = tg + ((wave - g - j - b) & 3);      // (two of four wavefronts with rows are not the same two everywhere)
@@ -586,11 +613,16 @@ __global__ __launch_bounds__(256, 2) void window_rows_ring(win_args a, int tile_
         row_tile<HD> t;
         load_rows<HD>(a, s, r0, nn, rt, j, all_lo, t, lane);
         begin_tile<HD>(t);
-        ring_keys<HD, false>(a, s, bt, j, k0, k_end, a.part_keys, all_lo, s.L, t, rt >= nrt, lds, [&]() __attribute__((always_inline)) {
-            put_partial<HD>(a, t, r0, rt, R, G, j, c, lane);
-            begin_tile<HD>(t);
-            c++;
-        });
+        if constexpr (WHOLE) {
+            ring_keys<HD, false>(a, s, bt, j, k0, k_end, INT32_MAX / 2, all_lo, s.L, t, rt >= nrt, lds, [&]() __attribute__((always_inline)) {});
+            put_result<HD>(a, t, r0, rt, R, G, j, lane);
+        } else {
+            ring_keys<HD, false>(a, s, bt, j, k0, k_end, a.part_keys, all_lo, s.L, t, rt >= nrt, lds, [&]() __attribute__((always_inline)) {
+                put_partial<HD>(a, t, r0, rt, R, G, j, c, lane);
+                begin_tile<HD>(t);
+                c++;
+            });
+        }
     }
 }
 
@@ -605,7 +637,7 @@ __global__ __launch_bounds__(256) void window_merge(win_args a) {
     const int lane = threadIdx.x & 63, head = (blockIdx.y * 4 + (threadIdx.x >> 6)) * HEADS + lane / LANES;
     if ((blockIdx.y * 4 + (threadIdx.x >> 6)) * HEADS >= a.hq) return;
     for (int row = blockIdx.x;; row += gridDim.x) {
-        const size_t prow = ((size_t)row * a.hq + min(head, a.hq - 1)) * a.max_parts;
+        const size_t prow = (size_t)row * a.hq + min(head, a.hq - 1);
         const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + prow;
         const _Float16* po = a.part_o + prow * HD + 8 * (lane % LANES);
         float2 x0[AHEAD];
@@ -614,8 +646,8 @@ __global__ __launch_bounds__(256) void window_merge(win_args a) {
             // (in bounds whether the row and its partitions exist or not: the grid is no larger than the workspace's rows)
 #pragma unroll
             for (int p = 0; p < AHEAD; p++) {
-                x0[p] = ml[min(p, a.max_parts - 1)];
-                v0[p] = *reinterpret_cast<const f16x8*>(po + (size_t)min(p, a.max_parts - 1) * HD);
+                x0[p] = ml[min(p, a.max_parts - 1) * a.part_rows];
+                v0[p] = *reinterpret_cast<const f16x8*>(po + min(p, a.max_parts - 1) * a.part_rows * HD);
             }
             hs_loads_issued();
         }
@@ -635,8 +667,8 @@ __global__ __launch_bounds__(256) void window_merge(win_args a) {
                     x[p] = p < n ? x0[p] : make_float2(-INFINITY, 0.f);
                     v[p] = v0[p];
                 } else {
-                    x[p] = ml[at];
-                    v[p] = *reinterpret_cast<const f16x8*>(po + (size_t)at * HD);
+                    x[p] = ml[at * a.part_rows];
+                    v[p] = *reinterpret_cast<const f16x8*>(po + at * a.part_rows * HD);
                 }
             }
             float m = top;
@@ -706,41 +738,45 @@ __global__ __launch_bounds__(256, 2) void window_chunk(win_args a, int nx) {
         begin_tile<HD>(t);
         ring_keys<HD, true>(a, s, bt, j, s.skip(0), k_end, INT32_MAX / 2, max(0, s.L + node1 + 1 - a.window), s.L + node0 + 1, t, rt * 32 >= R, lds,
                       [&]() __attribute__((always_inline)) {});
-        const float inv = t.l == 0.f ? 0.f : 1.f / t.l;
-        bf16_t* po = a.out + ((size_t)(r0 + node) * a.hq + j * G + (rho - node * G)) * HD;
-#pragma unroll
-        for (int dt = 0; dt < HD / 32; dt++)
-#pragma unroll
-            for (int g4 = 0; g4 < 4; g4++) {
-                if (rho >= R) break;
-                u32x2 x;
-                x.x = (uint32_t)to_bf16(t.o[dt][4 * g4] * inv) | ((uint32_t)to_bf16(t.o[dt][4 * g4 + 1] * inv) << 16);
-                x.y = (uint32_t)to_bf16(t.o[dt][4 * g4 + 2] * inv) | ((uint32_t)to_bf16(t.o[dt][4 * g4 + 3] * inv) << 16);
-                *reinterpret_cast<u32x2*>(po + dt * 32 + 8 * g4 + 4 * half) = x;
-            }
+        put_result<HD>(a, t, r0, rt, R, G, j, lane);
     }
 }
 
 // The most query rows per KV head that a draft can have.
 int rows_of(const hs_ctx* ctx) { return ctx->desc.n_q_heads / ctx->desc.n_kv_heads * (1 + ctx->lim.c_max * ctx->lim.k_max); }
 
-// Partitions of a draft's keys: their length, and the most that a sequence can have.  A function of the context's limits, the window
-// and the sinks, so that the order of a row's sums is the same in every step.
-struct win_plan { int part_keys, max_parts; };
+// How a draft's keys are taken.  A function of the context's limits, the window and the sinks, so that the order of a row's sums is the same in
+// every step.
+//
+// WIN_WHOLE: a workgroup per (sequence, KV head), which writes the result itself.  Where there are as many of these as compute units: partial
+// results in the middle of the key stream and the launch that joins them cost 256 drafts of 28 heads over 4096 keys 408 instead of 365 us, 64
+// trees of 40 heads over 2048 keys 130 instead of 101, 64 single tokens of 28 heads over 1024 keys 51 instead of 38, 64 drafts of 28 heads over
+// 4096 keys 119 instead of 117.  The limits do not say how many sequences there are now: 8 drafts within limits for 256 take 108 us instead of
+// 60.  Only up to 8192 keys, since a workgroup walks all that a sequence has (and its pages' numbers lie in LDS).
+//
+// WIN_FEW: a wavefront per partition, of limits with at most 32 query rows per KV head and two tiles of 32 keys for every SIMD: all of them are
+// on their way at once (8 single tokens of 28 heads over 1024 keys 20 us; by the ring 25; 32 of them 34 and 30).
+//
+// WIN_PARTS: otherwise; a workgroup per run of partitions, and a launch that joins them.
+enum { WIN_WHOLE, WIN_FEW, WIN_PARTS };
+constexpr int WIN_WHOLE_KEYS = 8192;
+struct win_plan { int kind, part_keys, max_parts; };
 win_plan plan_rows(const hs_ctx* ctx, int window, int sinks) {
     const long long cap = (long long)ctx->lim.max_blocks_per_seq * 16, nodes = 1 + ctx->lim.c_max * ctx->lim.k_max;
     const long long span = std::min<long long>(cap, window), s = std::min<long long>(cap, sinks);
+    const long long units = (long long)ctx->lim.max_batch * ctx->desc.n_kv_heads;
     auto most = [&](long long part) {
         return std::min((s + part - 1) / part + (span + nodes - 2) / part + 2, (cap + part - 1) / part);
     };
+    const int kind = span + s <= WIN_WHOLE_KEYS && units >= ctx->n_cu ? WIN_WHOLE
+                     : rows_of(ctx) <= 32 && units * (span + s) <= 64ll * 4 * ctx->n_cu ? WIN_FEW : WIN_PARTS;
     // Long partitions mean fewer partial results, which are written into the middle of the key stream; short ones keep a small batch spread
-    // over the chip: a wavefront each of a draft of few rows, a workgroup each of larger ones.
-    const bool wave = rows_of(ctx) <= 32;
-    long long part = wave ? 1024 : 2048;
-    while (part > 64 && (long long)ctx->lim.max_batch * ctx->desc.n_kv_heads * ((span + part - 1) / part) < (wave ? 1024 : 512)) part /= 2;
+    // over the chip: a wavefront or a workgroup each.
+    long long part = kind == WIN_FEW ? 1024 : 2048;
+    while (part > 64 && units * ((span + part - 1) / part) < (kind == WIN_FEW ? 1024 : 512)) part /= 2;
     while (part < ctx->att_part && most(part) > ctx->max_parts) part *= 2;      // (what the workspace holds)
     if (most(part) > ctx->max_parts) part = ctx->att_part;
-    return {(int)part, (int)most(part)};
+    return {kind, (int)part, (int)most(part)};
 }
 
 win_args make_args(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step, const void* q,
@@ -769,8 +805,11 @@ win_args make_args(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const
     a.sinks = sinks;
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)d.head_dim);
     const win_plan p = plan_rows(ctx, window, sinks);
+    a.kind = p.kind;
+    a.lag = rows_of(ctx) <= 32 ? 0.f : 8.f;
     a.part_keys = p.part_keys;
     a.max_parts = p.max_parts;
+    a.part_rows = (size_t)ctx->lim.max_rows * d.n_q_heads;
     return a;
 }
 
@@ -780,7 +819,7 @@ void hs_launch_window_attention(const hs_ctx* ctx, int layer, const hs_kv_cache*
                                 const void* q, void* out, int window, int sinks, hipStream_t st) {
     win_args a = make_args(ctx, layer, cache, seq, step, q, out, window, sinks);
     const int most = rows_of(ctx);
-    if (most <= 32) {
+    if (a.kind == WIN_FEW) {
         a.groups = (a.max_parts + 3) / 4;
         const dim3 grid((unsigned)(a.groups * a.hkv * a.batch));
         if (ctx->desc.head_dim == 128) hipLaunchKernelGGL((window_rows<128>), grid, dim3(256), 0, st, a);
@@ -791,7 +830,8 @@ void hs_launch_window_attention(const hs_ctx* ctx, int layer, const hs_kv_cache*
     // rounds of two workgroups per compute unit, of which each takes as long as WIN_START tiles until its first one is there.
     const int tile_groups = (most + 127) / 128;
     long long best = 0;
-    for (int groups = 1; groups <= a.max_parts; groups++) {
+    if (a.kind == WIN_WHOLE) a.groups = 1;
+    for (int groups = 1; a.kind != WIN_WHOLE && groups <= a.max_parts; groups++) {
         const int run = (a.max_parts + groups - 1) / groups * (a.part_keys / 32);
         if (run > WIN_RUN) continue;      // (one partition is at most 64 tiles)
         const long long rounds = ((long long)groups * a.hkv * a.batch + 2 * ctx->n_cu - 1) / (2 * ctx->n_cu);
@@ -799,13 +839,19 @@ void hs_launch_window_attention(const hs_ctx* ctx, int layer, const hs_kv_cache*
         if (a.groups == 0 || cost < best) { best = cost; a.groups = groups; }
     }
     const dim3 grid((unsigned)(a.groups * a.hkv * a.batch * tile_groups));
-    if (ctx->desc.head_dim == 128) hipLaunchKernelGGL((window_rows_ring<128>), grid, dim3(256), 0, st, a, tile_groups);
-    else hipLaunchKernelGGL((window_rows_ring<64>), grid, dim3(256), 0, st, a, tile_groups);
+    if (ctx->desc.head_dim == 128) {
+        if (a.kind == WIN_WHOLE) hipLaunchKernelGGL((window_rows_ring<128, true>), grid, dim3(256), 0, st, a, tile_groups);
+        else hipLaunchKernelGGL((window_rows_ring<128, false>), grid, dim3(256), 0, st, a, tile_groups);
+    } else {
+        if (a.kind == WIN_WHOLE) hipLaunchKernelGGL((window_rows_ring<64, true>), grid, dim3(256), 0, st, a, tile_groups);
+        else hipLaunchKernelGGL((window_rows_ring<64, false>), grid, dim3(256), 0, st, a, tile_groups);
+    }
 }
 
 void hs_launch_window_merge(const hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step, void* out,
                             int window, int sinks, hipStream_t st) {
     const win_args a = make_args(ctx, 0, cache, seq, step, nullptr, out, window, sinks);
+    if (a.kind == WIN_WHOLE) return;
     const int per = 4 * 512 / ctx->desc.head_dim, sets = (a.hq + per - 1) / per;      // heads of a workgroup, workgroups of a row
     const dim3 grid(hs_row_grid(ctx, 256, sets), sets);
     const bool early = ctx->lim.max_rows <= HS_EARLY_ROWS;
@@ -822,6 +868,7 @@ void hs_launch_window_chunk(const hs_ctx* ctx, int layer, const hs_kv_cache* cac
                             const hs_step* step, const void* q, void* out, int chunk, int window, int sinks, hipStream_t st) {
     win_args a = make_args(ctx, layer, cache, seq, step, q, out, window, sinks);
     a.seq_len = len_plus1;
+    a.lag = 8.f;
     // (a grid has fewer than 2^24 workgroups of 256: where that is too few, they take several blocks of rows)
     const long long most = std::max<long long>(1, (1ll << 23) / ((long long)a.hkv * a.batch));
     const int nx = (int)std::min(most, ((long long)chunk * (a.hq / a.hkv) + 127) / 128);

@@ -34,6 +34,20 @@ def test_single_tokens(heads, window, sinks):
     eng.close()
 
 
+@pytest.mark.parametrize("heads", [(28, 4, 128), (7, 1, 64), (4, 4, 64)])
+@pytest.mark.parametrize("window,sinks", [(1, 4), (2500, 0), (4000, 1100), (1 << 30, 0), (300, 1 << 30)])
+def test_single_tokens_behind_long_texts(heads, window, sinks):
+    """Several partitions per sequence, of few sequences."""
+    lens = [1, 4999, 2048, 2049, 3500] * (8 // heads[1])
+    eng = engine(*heads, lens, 1)
+    pars = [chain(0)] * len(lens)
+    m = lay_out(eng, lens, pars)
+    q = queries(m, eng)
+    eng.workspace.fill_(0xFF)
+    check(run(eng, m, q, window, sinks), eng, lens, pars, q, window, sinks)
+    eng.close()
+
+
 @pytest.mark.parametrize("heads", HEADS)
 @pytest.mark.parametrize("window,sinks", [(1, 0), (3, 0), (5, 2), (20, 4), (40, 600), (63, 1), (64, 1), (300, 4)])
 def test_drafts_and_trees(heads, window, sinks):
@@ -85,6 +99,34 @@ def test_large_scores():
     for scale in (0.0, 30.0):
         q = queries(m, eng, scale=scale)
         check(run(eng, m, q, 2500, 8), eng, lens, pars, q, 2500, 8)
+    eng.close()
+
+
+@pytest.mark.parametrize("heads,batch", [((8, 2, 64), 256), ((40, 8, 128), 64)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (20, 4), (64, 70), (300, 5), (8000, 8)])
+def test_large_batches(heads, batch, window, sinks):
+    """As many (sequence, KV head) pairs as a launch has places: a workgroup for each, which writes the result itself (up to 8192 keys in
+    sinks and window); some sequences without rows, in drafts of one to 17 nodes."""
+    rng = np.random.default_rng(window)
+    nodes = 17
+    lens = [int(x) for x in rng.integers(1, 700, batch)]
+    pars = [None if i % 7 == 3 else chain(0) if i % 3 == 0 else random_tree(int(rng.integers(2, nodes + 1)), rng) for i in range(batch)]
+    eng = engine(*heads, lens, nodes)
+    m = lay_out(eng, lens, pars)
+    q = queries(m, eng)
+    eng.workspace.fill_(0xFF)
+    out = run(eng, m, q, window, sinks)
+    check(out, eng, lens, pars, q, window, sinks)
+    # the output may be the queries, and a row's bits do not depend on its neighbours
+    buf = torch.full((eng.max_rows, q.shape[1]), 7.0, device="cuda:0", dtype=q.dtype)
+    buf[:m] = q
+    eng.attention_window(0, buf, buf, window, sinks)
+    assert torch.equal(buf, out)
+    alone = [p if p is None else chain(0) for p in pars]
+    starts = np.cumsum([0] + [0 if p is None else len(p) for p in pars])[:-1]
+    first = [int(s) for s, p in zip(starts, pars) if p is not None]
+    m = lay_out(eng, lens, alone)
+    assert torch.equal(run(eng, m, q[first], window, sinks)[:m], out[first])
     eng.close()
 
 
