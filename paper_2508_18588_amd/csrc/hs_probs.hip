@@ -76,7 +76,8 @@ __device__ __forceinline__ bool whole_pieces(const void* p, size_t stride) {
 }
 
 // ---- p[t] = exp((l[t] - max l) / T) / sum.  Bound by memory: the logits once and the probabilities once, and of the second reading of the
-// logits, when maximum and sum are known, what the caches don't have.
+// logits, when maximum and sum are known, what the caches don't have.  (1088 rows of 152064 tokens: 337 us, 3.9 TB/s of what has to move once, where
+// a copy reaches 4.9; seven rows of bf16: 12 us, two launches.)
 
 // Maximum and sum are those of units of 1024 tokens, a wavefront each, joined in their order: a row's probabilities have the same bits whatever
 // other rows there are and however the call is launched.
@@ -219,6 +220,8 @@ __global__ __launch_bounds__(256) void probs_write(probs_args p) {
 // slice of the vocabulary; the last one walks again with the sums at hand and looks for the token.  A walk that needs the sum of a rejected
 // child's node on its way takes a further launch of the first kind; more of these than were launched are summed by the last one alone.  (Where
 // the walk has come to is recorded, so that the last launch need not walk again as a rule: a chain of round trips to memory less.)
+// Bound by memory where batches are large, by the launches and their chains of round trips where they are small: 128 histories of 152064 tokens
+// 18 us for the sums (4.3 TB/s) and 6 for the pick, 64 trees twice 12 to 17 and 6; four drafts over 4096 tokens 5 and 6.
 constexpr int SLICE = HS_PROBS_SLICE, PER = SLICE / 256;
 
 struct verify_record;
