@@ -104,17 +104,19 @@ __device__ __forceinline__ bool take_nonfinite(bf16x8& x) {
 // The pages of a tile's keys; -1: there is none, or no row sees a key of it.
 struct places { int p0, p1; };
 
-// What a row sees of a tile that not every row sees all of: bit e of the result, for key e of the lane's.
+// What a row sees of a tile that not every row sees all of: bit e of the result, for key e of the lane's (two runs of eight keys).
+__device__ __forceinline__ unsigned below(int n) { return (1u << min(max(n, 0), 8)) - 1u; }      // of eight keys the first n
 template <int HD>
 __device__ __forceinline__ unsigned seen_keys(const win_args& a, const win_span& s, const row_tile<HD>& t, const places& here, int kb, int half) {
     unsigned seen = 0;
 #pragma unroll
-    for (int e = 0; e < 16; e++) {
-        const int key = kb + 16 * (e >> 3) + 8 * half + (e & 7), node = key - s.L;
-        // (no branches: the shift's amount is taken modulo 64, and a node's bit counts between 0 and 63)
-        const bool old = (key < t.hi) & ((key >= t.lo) | (key < a.sinks));
-        const bool vis = (old | (((unsigned)node < 64u) & (bool)((t.anc >> (node & 63)) & 1ull))) & ((e < 8 ? here.p0 : here.p1) >= 0);
-        seen |= (unsigned)vis << e;
+    for (int g = 0; g < 2; g++) {
+        const int base = kb + 16 * g + 8 * half, node = base - s.L;
+        const unsigned old = below(t.hi - base) & (~below(t.lo - base) | below(a.sinks - base));
+        // (no branches: a shift's amount is taken modulo 64)
+        const uint64_t up = t.anc >> (node & 63), down = t.anc << (-node & 63);
+        const unsigned nodes = (unsigned)node < 64u ? (unsigned)up : (unsigned)-node < 8u ? (unsigned)down : 0u;
+        seen |= ((g ? here.p1 : here.p0) >= 0 ? (old | nodes) & 0xFFu : 0u) << (8 * g);
     }
     return seen;
 }
@@ -135,7 +137,10 @@ __device__ __forceinline__ float take_scores(const win_args& a, const win_span& 
     if (masked) {
         const unsigned seen = seen_keys<HD>(a, s, t, here, kb, half);
 #pragma unroll
-        for (int e = 0; e < 16; e++) sc[e] = (seen >> e) & 1u ? sc[e] : -INFINITY;
+        for (int e = 0; e < 16; e++) {
+            const unsigned keep = (unsigned)((int)(seen << (31 - e)) >> 31);
+            sc[e] = __uint_as_float((__float_as_uint(sc[e]) & keep) | (0xFF800000u & ~keep));      // (-inf)
+        }
     }
     float tmax = sc[0];
 #pragma unroll
@@ -161,11 +166,25 @@ __device__ __forceinline__ float take_scores(const win_args& a, const win_span& 
 // were any (see add_odd).
 template <int HD>
 __device__ __forceinline__ bool mask_values(value_tile<HD>& v) {
+    // (an exponent of all ones and one in its last place go over into the sign's)
+    unsigned some = 0;
+#pragma unroll
+    for (int pp = 0; pp < 2; pp++)
+#pragma unroll
+        for (int dt = 0; dt < HD / 32; dt++) {
+            const u32x4 u = __builtin_bit_cast(u32x4, v.v[pp][dt]);
+#pragma unroll
+            for (int i = 0; i < 4; i++) some |= (u[i] & 0x7F807F80u) + 0x00800080u;
+        }
+    if (!__any((some & 0x80008000u) != 0)) return false;
     bool odd = false;
 #pragma unroll
     for (int pp = 0; pp < 2; pp++)
 #pragma unroll
-        for (int dt = 0; dt < HD / 32; dt++) odd |= take_nonfinite(v.v[pp][dt]);
+        for (int dt = 0; dt < HD / 32; dt++) {
+            odd |= take_nonfinite(v.v[pp][dt]);
+            asm volatile("" : "+v"(v.v[pp][dt]));
+        }
     return odd;
 }
 // Probabilities of a tile, as the second product's operand, and their sum.
@@ -553,12 +572,6 @@ __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, 
                     v.v[pp][dt] = *reinterpret_cast<const bf16x8*>(lds.ring + slot * T::BYTES + T::V + pp * T::PAGE + dt * 1024 + T::v_at(l32, half));
             if (masked) {
                 odd |= __any(mask_values<HD>(v));
-                // (changed in place: without this the values of all tiles were copied to where the masked ones end up, 432 -> 420 us for 256
-                // drafts over 4096 keys)
-#pragma unroll
-                for (int pp = 0; pp < 2; pp++)
-#pragma unroll
-                    for (int dt = 0; dt < NDT; dt++) asm volatile("" : "+v"(v.v[pp][dt]));
             }
             bf16x8 pb[2];
             // (the matrix unit goes to the wavefront that has products for it, 113 -> 107 us for 8 x 512 tokens, 28 heads, 1024 keys)
