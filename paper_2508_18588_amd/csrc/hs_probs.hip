@@ -13,75 +13,62 @@ __device__ __forceinline__ float wide(bf16_t v) { return bf16_to_f32(v); }
 __device__ __forceinline__ void narrow(float v, float& to) { to = v; }
 __device__ __forceinline__ void narrow(float v, bf16_t& to) { to = __builtin_isnan(v) ? (bf16_t)0x7FC0 : f32_to_bf16(v); }
 
-// Eight tokens from i on, as 32-bit values; `rest` beyond the row's n.  whole: 16-byte accesses are possible (i is a multiple of eight).
+// Rows are read and written in runs of 16 bytes of the logits, a wavefront's side by side: with eight values of 32 bits per lane, in two halves,
+// every access of the wavefront's touched half of twice as many sectors (1088 rows of 152064 tokens 336 -> 316 us).
 // (Stores are non-temporal: what they would take of the caches is better used by logits that are read again, 390 -> 357 us for 1088 rows of
 // 152064 tokens when a workgroup read all of its row twice.)
-constexpr int PIECE = 8;
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ void load_piece(const float* __restrict__ row, int i, int n, bool whole, float rest, float (&v)[PIECE]) {
-    if (whole && i + PIECE <= n) {
+template <typename T> constexpr int run_of = 16 / sizeof(T);
+// PER tokens, in runs that begin at from, from + step, ...  all: 16-byte accesses are possible, and all of the tokens are in the row (the same for
+// the wavefront: its loads are issued one after the other, without branches between them).
+template <int PER, typename T>
+__device__ __forceinline__ void load_runs(const T* __restrict__ row, int from, int step, int n, bool all, float rest, float (&v)[PER]) {
+    constexpr int RUN = run_of<T>;
+    if (all) {
+        typedef T run_t __attribute__((ext_vector_type(RUN)));
 #pragma unroll
-        for (int e = 0; e < PIECE; e += 4) {
-            const float4 x = *reinterpret_cast<const float4*>(row + i + e);
-            v[e] = x.x; v[e + 1] = x.y; v[e + 2] = x.z; v[e + 3] = x.w;
+        for (int u = 0; u < PER / RUN; u++) {
+            const run_t x = *reinterpret_cast<const run_t*>(row + from + u * step);
+#pragma unroll
+            for (int e = 0; e < RUN; e++) v[u * RUN + e] = wide((T)x[e]);
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < PIECE; e++) v[e] = i + e < n ? row[i + e] : rest;
+        for (int j = 0; j < PER; j++) {
+            const int i = from + j / RUN * step + j % RUN;
+            v[j] = i < n ? wide(row[i]) : rest;
+        }
     }
 }
-__device__ __forceinline__ void load_piece(const bf16_t* __restrict__ row, int i, int n, bool whole, float rest, float (&v)[PIECE]) {
-    if (whole && i + PIECE <= n) {
-        const uint4 x = *reinterpret_cast<const uint4*>(row + i);
-        const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+template <int RUN, typename T>
+__device__ __forceinline__ void store_run(T* __restrict__ row, int i, int n, bool whole, const float* v) {
+    if (whole && i + RUN <= n) {
+        constexpr int N = RUN < run_of<T> ? RUN : run_of<T>;      // (bf16 made of floats: 8 bytes; floats made of bf16: twice 16)
+        typedef T run_t __attribute__((ext_vector_type(N)));
 #pragma unroll
-        for (int e = 0; e < PIECE; e += 2) {
-            v[e] = __uint_as_float(u[e / 2] << 16);
-            v[e + 1] = __uint_as_float(u[e / 2] & 0xFFFF0000u);
+        for (int k = 0; k < RUN; k += N) {
+            run_t x;
+#pragma unroll
+            for (int e = 0; e < N; e++) { T y; narrow(v[k + e], y); x[e] = y; }
+            __builtin_nontemporal_store(x, reinterpret_cast<run_t*>(row + i + k));
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < PIECE; e++) v[e] = i + e < n ? wide(row[i + e]) : rest;
-    }
-}
-__device__ __forceinline__ void store_piece(float* __restrict__ row, int i, int n, bool whole, const float (&v)[PIECE]) {
-    if (whole && i + PIECE <= n) {
-#pragma unroll
-        for (int e = 0; e < PIECE; e += 4) __builtin_nontemporal_store(f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]}, reinterpret_cast<f32x4*>(row + i + e));
-    } else {
-#pragma unroll
-        for (int e = 0; e < PIECE; e++)
-            if (i + e < n) row[i + e] = v[e];
-    }
-}
-__device__ __forceinline__ void store_piece(bf16_t* __restrict__ row, int i, int n, bool whole, const float (&v)[PIECE]) {
-    bf16_t b[PIECE];
-#pragma unroll
-    for (int e = 0; e < PIECE; e++) narrow(v[e], b[e]);
-    if (whole && i + PIECE <= n) {
-        u32x4 u;
-#pragma unroll
-        for (int e = 0; e < 4; e++) u[e] = (uint32_t)b[2 * e] | (uint32_t)b[2 * e + 1] << 16;
-        __builtin_nontemporal_store(u, reinterpret_cast<u32x4*>(row + i));
-    } else {
-#pragma unroll
-        for (int e = 0; e < PIECE; e++)
-            if (i + e < n) row[i + e] = b[e];
+        for (int e = 0; e < RUN; e++)
+            if (i + e < n) narrow(v[e], row[i + e]);
     }
 }
 template <typename T>
-__device__ __forceinline__ bool whole_pieces(const void* p, size_t stride) {
+__device__ __forceinline__ bool whole_runs(const void* p, size_t stride) {
     return (((unsigned long long)p | stride * sizeof(T)) & 15ull) == 0;
 }
 
 // ---- p[t] = exp((l[t] - max l) / T) / sum.  Bound by memory: the logits once and the probabilities once, and of the second reading of the
-// logits, when maximum and sum are known, what the caches don't have.  (1088 rows of 152064 tokens: 337 us, 3.9 TB/s of what has to move once, where
+// logits, when maximum and sum are known, what the caches don't have.  (1088 rows of 152064 tokens: 315 us, 4.2 TB/s of what has to move once, where
 // a copy reaches 4.9; seven rows of bf16: 12 us, two launches.)
 
 // Maximum and sum are those of units of 1024 tokens, a wavefront each, joined in their order: a row's probabilities have the same bits whatever
 // other rows there are and however the call is launched.
-constexpr int UNIT = 1024, UNIT_PIECES = UNIT / 64 / PIECE;
+constexpr int UNIT = 1024, UNIT_PER = UNIT / 64;
 struct probs_args {
     const void* logits;
     void* out;
@@ -110,23 +97,18 @@ __device__ __forceinline__ float wave_sum_f32(float v) {
     step(lane_xor<1>(__float_as_uint(v)));
     return v;
 }
-// A wavefront's unit of a row (tokens beyond the vocabulary: -inf), and what goes into the sums.
+// A wavefront's unit of a row (tokens beyond the vocabulary: -inf), run k of lane l at (64 k + l) RUN, and what goes into the sums.
 template <typename T>
-__device__ __forceinline__ void load_unit(const T* l, int unit, int lane, const probs_args& p, bool whole, float (&v)[UNIT_PIECES][PIECE]) {
-#pragma unroll
-    for (int u = 0; u < UNIT_PIECES; u++) load_piece(l, unit * UNIT + (lane + 64 * u) * PIECE, p.vocab, whole, -INFINITY, v[u]);
+__device__ __forceinline__ void load_unit(const T* l, int unit, int lane, const probs_args& p, bool whole, float (&v)[UNIT_PER]) {
+    load_runs(l, unit * UNIT + lane * run_of<T>, 64 * run_of<T>, p.vocab, whole && (unit + 1) * UNIT <= p.vocab, -INFINITY, v);
 }
-__device__ __forceinline__ float2 unit_stat(const float (&v)[UNIT_PIECES][PIECE], const probs_args& p) {
+__device__ __forceinline__ float2 unit_stat(const float (&v)[UNIT_PER], const probs_args& p) {
     float m = -INFINITY, s = 0.f;
 #pragma unroll
-    for (int u = 0; u < UNIT_PIECES; u++)
-#pragma unroll
-        for (int e = 0; e < PIECE; e++) m = fmaxf(m, v[u][e]);
+    for (int e = 0; e < UNIT_PER; e++) m = fmaxf(m, v[e]);
     m = wave_max_f32(m);
 #pragma unroll
-    for (int u = 0; u < UNIT_PIECES; u++)
-#pragma unroll
-        for (int e = 0; e < PIECE; e++) s += v[u][e] == -INFINITY ? 0.f : weight(v[u][e], m, p.c_hi, p.c_lo);
+    for (int e = 0; e < UNIT_PER; e++) s += v[e] == -INFINITY ? 0.f : weight(v[e], m, p.c_hi, p.c_lo);
     return make_float2(m, wave_sum_f32(s));
 }
 // The row's largest logit, and 1 / the sum of its weights, by a wavefront from the units'.
@@ -141,13 +123,14 @@ __device__ __forceinline__ float2 join_units(const float2* stats, const probs_ar
     s = wave_sum_f32(s);
     return make_float2(m, s == 0.f ? 0.f : 1.f / s);
 }
-template <typename T>
-__device__ __forceinline__ void store_unit(T* o, int unit, int lane, const probs_args& p, bool whole, float (&v)[UNIT_PIECES][PIECE], float2 top) {
+template <typename TI, typename T>
+__device__ __forceinline__ void store_unit(T* o, int unit, int lane, const probs_args& p, bool whole, float (&v)[UNIT_PER], float2 top) {
+    constexpr int RUN = run_of<TI>;
 #pragma unroll
-    for (int u = 0; u < UNIT_PIECES; u++) {
+    for (int k = 0; k < UNIT_PER / RUN; k++) {
 #pragma unroll
-        for (int e = 0; e < PIECE; e++) v[u][e] = (v[u][e] == -INFINITY ? 0.f : weight(v[u][e], top.x, p.c_hi, p.c_lo)) * top.y;
-        store_piece(o, unit * UNIT + (lane + 64 * u) * PIECE, p.vocab, whole, v[u]);
+        for (int e = k * RUN; e < (k + 1) * RUN; e++) v[e] = (v[e] == -INFINITY ? 0.f : weight(v[e], top.x, p.c_hi, p.c_lo)) * top.y;
+        store_run<RUN>(o, unit * UNIT + (64 * k + lane) * RUN, p.vocab, whole, v + k * RUN);
     }
 }
 
@@ -160,13 +143,13 @@ __global__ __launch_bounds__(1024) void probs_rows(probs_args p) {
     __shared__ float2 stats[ROW_UNITS];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int M = p.live ? min(*p.live, p.rows) : p.rows;
-    const bool in_whole = whole_pieces<TI>(p.logits, p.logits_stride), out_whole = whole_pieces<TO>(p.out, p.out_stride);
+    const bool in_whole = whole_runs<TI>(p.logits, p.logits_stride), out_whole = whole_runs<TO>(p.out, p.out_stride);
     for (int row = blockIdx.x; row < M; row += gridDim.x) {
         const TI* l = (const TI*)p.logits + row * p.logits_stride;
         TO* o = (TO*)p.out + row * p.out_stride;
         __syncthreads();      // (the row before has been read)
         for (int k = wave; k < p.units; k += 32) {
-            float v[2][UNIT_PIECES][PIECE];
+            float v[2][UNIT_PER];
             load_unit(l, k, lane, p, in_whole, v[0]);
             if (k + 16 < p.units) load_unit(l, k + 16, lane, p, in_whole, v[1]);
             float2 x = unit_stat(v[0], p);
@@ -180,9 +163,9 @@ __global__ __launch_bounds__(1024) void probs_rows(probs_args p) {
         const float2 top = join_units(stats, p, lane);
         for (int k = (p.units - 1) / 16 * 16 + wave; k >= 0; k -= 16) {
             if (k >= p.units) continue;
-            float v[UNIT_PIECES][PIECE];
+            float v[UNIT_PER];
             load_unit(l, k, lane, p, in_whole, v);
-            store_unit(o, k, lane, p, out_whole, v, top);
+            store_unit<TI>(o, k, lane, p, out_whole, v, top);
         }
     }
 }
@@ -193,8 +176,8 @@ __global__ __launch_bounds__(256) void probs_stats(probs_args p) {
     const int groups = (p.units + 3) / 4, row = blockIdx.x / groups, lane = threadIdx.x & 63;
     const int unit = blockIdx.x % groups * 4 + (threadIdx.x >> 6);
     if (unit >= p.units || (p.live && p.first + row >= *p.live)) return;
-    float v[UNIT_PIECES][PIECE];
-    load_unit((const TI*)p.logits + row * p.logits_stride, unit, lane, p, whole_pieces<TI>(p.logits, p.logits_stride), v);
+    float v[UNIT_PER];
+    load_unit((const TI*)p.logits + row * p.logits_stride, unit, lane, p, whole_runs<TI>(p.logits, p.logits_stride), v);
     const float2 x = unit_stat(v, p);
     if (lane == 0) p.stats[(size_t)row * p.units + unit] = x;
 }
@@ -203,10 +186,10 @@ __global__ __launch_bounds__(256) void probs_write(probs_args p) {
     const int groups = (p.units + 3) / 4, row = blockIdx.x / groups, lane = threadIdx.x & 63;
     const int unit = blockIdx.x % groups * 4 + (threadIdx.x >> 6);
     if (unit >= p.units || (p.live && p.first + row >= *p.live)) return;
-    float v[UNIT_PIECES][PIECE];
-    load_unit((const TI*)p.logits + row * p.logits_stride, unit, lane, p, whole_pieces<TI>(p.logits, p.logits_stride), v);
+    float v[UNIT_PER];
+    load_unit((const TI*)p.logits + row * p.logits_stride, unit, lane, p, whole_runs<TI>(p.logits, p.logits_stride), v);
     const float2 top = join_units(p.stats + (size_t)row * p.units, p, lane);
-    store_unit((TO*)p.out + row * p.out_stride, unit, lane, p, whole_pieces<TO>(p.out, p.out_stride), v, top);
+    store_unit<TI>((TO*)p.out + row * p.out_stride, unit, lane, p, whole_runs<TO>(p.out, p.out_stride), v, top);
 }
 
 // ---- verification.  At a node with the target's probabilities p and the draft's q: w_0 = p, Z_0 = 1; the children are tried in node
@@ -328,33 +311,32 @@ struct alignas(16) verify_record {
 };
 static_assert(sizeof(verify_record) <= HS_PROBS_RECORD, "the workspace's share");
 
-// What is left of the weights of a thread's tokens after r rejections at a node: pieces of eight tokens, the first at `from`, `step` apart.
+// What is left of the weights of a thread's tokens in a slice after r rejections at a node: runs of tokens, the first at `from`, `step` apart.
 template <typename T>
-__device__ __forceinline__ void weights_left(const verify_args& a, int row, int from, int step, int r, const verify_left& l, double (&w)[PER]) {
+__device__ __forceinline__ void weights_left(const verify_args& a, int row, int slice, int from, int step, int r, const verify_left& l, double (&w)[PER]) {
+    constexpr int RUN = run_of<T>;
     const bool point = a.q == nullptr, draft = !point && r > 0;
-    const bool pv = whole_pieces<T>(a.p, a.p_stride), qv = whole_pieces<T>(a.q, a.q_stride);
+    const bool pv = whole_runs<T>(a.p, a.p_stride), qv = whole_runs<T>(a.q, a.q_stride);
     const T *pr = (const T*)a.p + row * a.p_stride, *qr = (const T*)a.q + row * a.q_stride;
-    float p[PER / PIECE][PIECE], q[PER / PIECE][PIECE] = {};
+    float p[PER], q[PER] = {};
+    const bool inside = (slice + 1) * SLICE <= a.vocab;
+    load_runs(pr, from, step, a.vocab, pv && inside, 0.f, p);
+    if (draft) load_runs(qr, from, step, a.vocab, qv && inside, 0.f, q);
 #pragma unroll
-    for (int u = 0; u < PER / PIECE; u++) {
-        load_piece(pr, from + u * step, a.vocab, pv, 0.f, p[u]);
-        if (draft) load_piece(qr, from + u * step, a.vocab, qv, 0.f, q[u]);
-    }
-#pragma unroll
-    for (int j = 0; j < PER; j++) w[j] = counted(p[j / PIECE][j % PIECE]);
+    for (int j = 0; j < PER; j++) w[j] = counted(p[j]);
     for (int k = 0; k < r; k++) {
         const double z = l.z[k];
         const int rej = l.rej[k];
 #pragma unroll
         for (int j = 0; j < PER; j++)
-            w[j] = point ? (rej == from + j / PIECE * step + j % PIECE ? 0.0 : w[j]) : fmax(w[j] - z * counted(q[j / PIECE][j % PIECE]), 0.0);
+            w[j] = point ? (rej == from + j / RUN * step + j % RUN ? 0.0 : w[j]) : fmax(w[j] - z * counted(q[j]), 0.0);
     }
 }
 // Sum of one slice's weights, by the workgroup.
 template <typename T>
 __device__ __forceinline__ double sum_slice(const verify_args& a, int row, int slice, int r, const verify_left& l, double* red) {
     double w[PER], s = 0.0;
-    weights_left<T>(a, row, slice * SLICE + (int)threadIdx.x * PIECE, 256 * PIECE, r, l, w);
+    weights_left<T>(a, row, slice, slice * SLICE + (int)threadIdx.x * run_of<T>, 256 * run_of<T>, r, l, w);
 #pragma unroll
     for (int j = 0; j < PER; j++) s += w[j];
     return block_sum_f64(s, red);
@@ -476,7 +458,7 @@ __global__ __launch_bounds__(256) void verify_pick(verify_args a) {
         // PER consecutive tokens per thread: the first thread whose running sum exceeds the target holds the token
         const int lo = slice * SLICE + tid * PER;
         double w[PER], sum = 0.0;
-        weights_left<T>(a, r0 + s.cur, lo, PIECE, s.r, left, w);
+        weights_left<T>(a, r0 + s.cur, slice, lo, run_of<T>, s.r, left, w);
 #pragma unroll
         for (int j = 0; j < PER; j++) sum += w[j];
         const double incl = wave_prefix_f64(sum, lane);
