@@ -15,9 +15,9 @@
 //
 // A draft's rows are few and its keys many, and memory bounds it.  Four row tiles share a stream of key tiles through LDS; a workgroup walks all
 // keys of a (sequence, KV head), or a run of partitions, whose results a launch of its own joins (see plan_rows).  128 single tokens, 28 heads,
-// 1024 keys: 54 us, 5.0 TB/s (a copy reaches 4.9); 256 drafts, 4096 keys: 365 us, 5.1 TB/s; 64 trees of 17 nodes, 40 heads, 2048 keys: 101 us, 5.6
-// TB/s; the stream alone, without products, 319 and 95 us.  A chunk's rows are many: a workgroup takes 128 of them through all their keys (8 x
-// 512 tokens, 28 heads, 1024 keys: 100 us, 600 TFLOP/s of the 1215 that a large product of matrices reaches; matrix unit, vector unit and LDS are
+// 1024 keys: 51 us, 5.3 TB/s (a copy reaches 4.9); 256 drafts, 4096 keys: 360 us, 5.2 TB/s; 64 trees of 17 nodes, 40 heads, 2048 keys: 97 us, 5.8
+// TB/s; the stream alone, without products, 319 and 95 us when these took 412 and 131.  A chunk's rows are many: a workgroup takes 128 of them through
+// all their keys (8 x 512 tokens, 28 heads, 1024 keys: 94 us, 640 TFLOP/s of the 1215 that a large product of matrices reaches; matrix unit, vector unit and LDS are
 // each busy for two fifths of the time, with two wavefronts per SIMD to overlap them).
 //
 // Every sum has an order that depends on absolute key positions only (32-key tiles, partitions of part_keys, if any, merged in index order;
@@ -765,14 +765,16 @@ int rows_of(const hs_ctx* ctx) { return ctx->desc.n_q_heads / ctx->desc.n_kv_hea
 // results in the middle of the key stream and the launch that joins them cost 256 drafts of 28 heads over 4096 keys 408 instead of 365 us, 64
 // trees of 40 heads over 2048 keys 130 instead of 101, 64 single tokens of 28 heads over 1024 keys 51 instead of 38, 64 drafts of 28 heads over
 // 4096 keys 119 instead of 117.  The limits do not say how many sequences there are now: 8 drafts within limits for 256 take 108 us instead of
-// 60.  Only up to 8192 keys, since a workgroup walks all that a sequence has (and its pages' numbers lie in LDS).
+// 60.  Only up to 8192 keys, since a workgroup walks all that a sequence has (and its pages' numbers lie in LDS).  With fewer sequences, too,
+// where the walk is shorter than a second launch takes (8 single tokens over 68 keys 13.1 us instead of 14.7, 128 keys 14.4 and 15.1, 256 keys 17.4
+// and 15.4; 8 drafts 13.2 and 15.4, 14.3 and 16.2, 17.4 and 17.2).
 //
 // WIN_FEW: a wavefront per partition, of limits with at most 32 query rows per KV head and two tiles of 32 keys for every SIMD: all of them are
 // on their way at once (8 single tokens of 28 heads over 1024 keys 20 us; by the ring 25; 32 of them 34 and 30).
 //
 // WIN_PARTS: otherwise; a workgroup per run of partitions, and a launch that joins them.
 enum { WIN_WHOLE, WIN_FEW, WIN_PARTS };
-constexpr int WIN_WHOLE_KEYS = 8192;
+constexpr int WIN_WHOLE_KEYS = 8192, WIN_SHORT_KEYS = 160;
 struct win_plan { int kind, part_keys, max_parts; };
 win_plan plan_rows(const hs_ctx* ctx, int window, int sinks) {
     const long long cap = (long long)ctx->lim.max_blocks_per_seq * 16, nodes = 1 + ctx->lim.c_max * ctx->lim.k_max;
@@ -781,7 +783,7 @@ win_plan plan_rows(const hs_ctx* ctx, int window, int sinks) {
     auto most = [&](long long part) {
         return std::min((s + part - 1) / part + (span + nodes - 2) / part + 2, (cap + part - 1) / part);
     };
-    const int kind = span + s <= WIN_WHOLE_KEYS && units >= ctx->n_cu ? WIN_WHOLE
+    const int kind = span + s <= (units >= ctx->n_cu ? WIN_WHOLE_KEYS : WIN_SHORT_KEYS) ? WIN_WHOLE
                      : rows_of(ctx) <= 32 && units * (span + s) <= 64ll * 4 * ctx->n_cu ? WIN_FEW : WIN_PARTS;
     // Long partitions mean fewer partial results, which are written into the middle of the key stream; short ones keep a small batch spread
     // over the chip: a wavefront or a workgroup each.
