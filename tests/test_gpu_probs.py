@@ -321,6 +321,53 @@ def test_probabilities_that_are_none():
         eng.close()
 
 
+def test_a_very_large_vocabulary():
+    """More units and slices than a workgroup keeps or a wavefront has lanes for."""
+    vocab, m = 5000003, 6
+    rng = np.random.default_rng(6)
+    eng = engine(1, 1, 64, [8, 8], 3, vocab=vocab)
+    p, q = distributions(m, vocab, 5.0, 0.5, torch.float32, 4)
+    out = torch.empty(m, vocab, device="cuda:0")
+    x = torch.randn(m, vocab, device="cuda:0") * 3
+    eng.probs(x, out, 0.9)
+    e = torch.exp((x.double() - x.double().amax(-1, keepdim=True)) / 0.9)
+    # (as in _check_probs, with sums of 5000 units, 78 of them one after the other per lane)
+    want = e / e.sum(-1, keepdim=True)
+    assert ((out.double() - want).abs() <= want * 2.0 ** -24 * 300 + 2.0 ** -125).all()
+    pars = [chain(2), np.asarray([-1, 0, 0])]
+    toks = drafted(pars, q, vocab, rng)
+    for _ in range(3):
+        check(eng, pars, toks, p, q, uniforms(rng, m), uniforms(rng, 2))
+        check(eng, pars, toks, p, None, uniforms(rng, m), uniforms(rng, 2))
+    eng.close()
+
+
+def test_rows_far_apart():
+    """Rows whose places pass 32 bits, in elements and in bytes."""
+    vocab, m, far = 1003, 3, (1 << 30) + 24
+    rng = np.random.default_rng(5)
+    stores = [torch.empty(far * (m - 1) + vocab, device="cuda:0", dtype=torch.bfloat16) for _ in range(2)]
+    p, q = [t.as_strided((m, vocab), (far, 1)) for t in stores]
+    near = distributions(m, vocab, 4.0, 0.7, torch.bfloat16, 3)
+    x = torch.randn(m, vocab, device="cuda:0").to(torch.bfloat16)
+    eng = engine(1, 1, 64, [8], m, vocab=vocab)
+    p.copy_(x)
+    eng.probs(p, q, 0.7)
+    want = torch.empty_like(x)
+    eng.probs(x, want, 0.7)
+    assert torch.equal(q, want)
+    p.copy_(near[0])
+    q.copy_(near[1])
+    pars = [chain(m - 1)]
+    toks = drafted(pars, near[1], vocab, rng)
+    for _ in range(4):
+        ua, us = uniforms(rng, m), uniforms(rng, 1)
+        check(eng, pars, toks, p, q, ua, us)
+        check(eng, pars, toks, p, None, ua, us)
+    check(eng, pars, toks, p, q, np.zeros(m), uniforms(rng, 1))      # (all accepted: the last row)
+    eng.close()
+
+
 def test_children_with_the_same_token():
     rng, vocab, n = np.random.default_rng(4), 300, 16
     eng = engine(1, 1, 64, [8] * n, 9, vocab=vocab, c_max=2)

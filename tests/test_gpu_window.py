@@ -91,6 +91,20 @@ def test_chunks(heads, window, sinks, chunk):
     eng.close()
 
 
+def test_a_cache_of_more_than_four_gigabytes():
+    """17 texts of 131072 tokens in shuffled pages: offsets beyond 32 bits, whole walks, wavefronts', partitions and a chunk."""
+    n, nodes, batch = 131072, 5, 17
+    lens = [n - 3 * i for i in range(batch)]
+    eng = engine(8, 8, 128, lens, nodes)
+    assert eng.kc.numel() * 2 > 1 << 32
+    pars = [chain(nodes - 1)] * batch
+    for window, sinks, chunk in ((100, 4, 0), (300, 5, 0), (5000, 40, 0), (300, 5, nodes)):
+        m = lay_out_chunk(eng, [nodes] * batch) if chunk else lay_out(eng, lens, pars)
+        q = queries(m, eng)
+        check(run(eng, m, q, window, sinks, chunk), eng, lens, pars, q, window, sinks, chunk=bool(chunk))
+    eng.close()
+
+
 def test_large_scores():
     """Scores of a few hundred (one key has all the weight) and a long window over many partitions."""
     lens, pars = [3000, 2999], [chain(4), chain(0)]
