@@ -765,16 +765,18 @@ int rows_of(const hs_ctx* ctx) { return ctx->desc.n_q_heads / ctx->desc.n_kv_hea
 // results in the middle of the key stream and the launch that joins them cost 256 drafts of 28 heads over 4096 keys 408 instead of 365 us, 64
 // trees of 40 heads over 2048 keys 130 instead of 101, 64 single tokens of 28 heads over 1024 keys 51 instead of 38, 64 drafts of 28 heads over
 // 4096 keys 119 instead of 117.  The limits do not say how many sequences there are now: 8 drafts within limits for 256 take 108 us instead of
-// 60.  Only up to 8192 keys, since a workgroup walks all that a sequence has (and its pages' numbers lie in LDS).  With fewer sequences, too,
-// where the walk is shorter than a second launch takes (8 single tokens over 68 keys 13.1 us instead of 14.7, 128 keys 14.4 and 15.1, 256 keys 17.4
-// and 15.4; 8 drafts 13.2 and 15.4, 14.3 and 16.2, 17.4 and 17.2).
+// 60.  Only up to 16000 keys, since a workgroup walks all that a sequence has (and its pages' numbers lie in LDS): texts of 2048 to 16384 tokens, 128
+// drafts of 28 heads over 8000 keys 317 us instead of 398, 15000 keys 494 and 589; 64 drafts behind up to 20000 tokens 197 and 225, 354 and 334.
+// With fewer sequences, too, where the walk is shorter than a second launch takes (8 single tokens over 68 keys 13.1 us instead of 14.7, 128 keys
+// 14.4 and 15.1, 256 keys 17.4 and 15.4; 8 drafts 13.2 and 15.4, 14.3 and 16.2, 17.4 and 17.2).
 //
 // WIN_FEW: a wavefront per partition, of limits with at most 32 query rows per KV head and two tiles of 32 keys for every SIMD: all of them are
 // on their way at once (8 single tokens of 28 heads over 1024 keys 20 us; by the ring 25; 32 of them 34 and 30).
 //
 // WIN_PARTS: otherwise; a workgroup per run of partitions, and a launch that joins them.
 enum { WIN_WHOLE, WIN_FEW, WIN_PARTS };
-constexpr int WIN_WHOLE_KEYS = 8192, WIN_SHORT_KEYS = 160;
+constexpr int WIN_WHOLE_KEYS = 16000, WIN_SHORT_KEYS = 160;
+static_assert(WIN_WHOLE_KEYS + HS_MAX_NODES + 4 * 32 <= 32 * WIN_RUN, "a walk's pages");
 struct win_plan { int kind, part_keys, max_parts; };
 win_plan plan_rows(const hs_ctx* ctx, int window, int sinks) {
     const long long cap = (long long)ctx->lim.max_blocks_per_seq * 16, nodes = 1 + ctx->lim.c_max * ctx->lim.k_max;

@@ -91,6 +91,18 @@ def test_chunks(heads, window, sinks, chunk):
     eng.close()
 
 
+@pytest.mark.parametrize("window,sinks", [(15900, 100), (15000, 1001)])
+def test_long_walks(window, sinks):
+    """One walk over as many keys as there are in a workgroup's list of pages, and one more than that in partitions."""
+    lens = [16300, 40, 18000] + [33] * 253
+    eng = engine(8, 1, 64, lens, 9)
+    pars = [chain(8), chain(3), chain(0)] + [chain(1)] * 253
+    m = lay_out(eng, lens, pars)
+    q = queries(m, eng)
+    check(run(eng, m, q, window, sinks), eng, lens, pars, q, window, sinks)
+    eng.close()
+
+
 def test_a_cache_of_more_than_four_gigabytes():
     """17 texts of 131072 tokens in shuffled pages: offsets beyond 32 bits, whole walks, wavefronts', partitions and a chunk."""
     n, nodes, batch = 131072, 5, 17
@@ -119,7 +131,7 @@ def test_large_scores():
 @pytest.mark.parametrize("heads,batch", [((8, 2, 64), 256), ((40, 8, 128), 64)])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (20, 4), (64, 70), (300, 5), (8000, 8)])
 def test_large_batches(heads, batch, window, sinks):
-    """As many (sequence, KV head) pairs as a launch has places: a workgroup for each, which writes the result itself (up to 8192 keys in
+    """As many (sequence, KV head) pairs as a launch has places: a workgroup for each, which writes the result itself (up to 16000 keys in
     sinks and window); some sequences without rows, in drafts of one to 17 nodes."""
     rng = np.random.default_rng(window)
     nodes = 17
