@@ -16,9 +16,9 @@
 // A draft's rows are few and its keys many, and memory bounds it.  Four row tiles share a stream of key tiles through LDS; a workgroup walks all
 // keys of a (sequence, KV head), or a run of partitions, whose results a launch of its own joins (see plan_rows).  128 single tokens, 28 heads,
 // 1024 keys: 51 us, 5.3 TB/s (a copy reaches 4.9); 256 drafts, 4096 keys: 360 us, 5.2 TB/s; 64 trees of 17 nodes, 40 heads, 2048 keys: 97 us, 5.8
-// TB/s; the stream alone, without products, 319 and 95 us when these took 412 and 131.  A chunk's rows are many: a workgroup takes 128 of them through
-// all their keys (8 x 512 tokens, 28 heads, 1024 keys: 94 us, 640 TFLOP/s of the 1215 that a large product of matrices reaches; matrix unit, vector unit and LDS are
-// each busy for two fifths of the time, with two wavefronts per SIMD to overlap them).
+// TB/s; the stream alone, without products, 319 and 95 us when these took 412 and 131.  A chunk's rows are many: a workgroup takes 128 of them
+// through all their keys (8 x 512 tokens, 28 heads, 1024 keys: 94 us, 640 TFLOP/s of the 1215 that a large product of matrices reaches; matrix unit,
+// vector unit and LDS are each busy for two fifths of the time, with two wavefronts per SIMD to overlap them).
 //
 // Every sum has an order that depends on absolute key positions only (32-key tiles, partitions of part_keys, if any, merged in index order;
 // keys that a row does not see contribute exact zeros): a row's result does not depend on what other rows are computed with it.
@@ -408,7 +408,7 @@ __device__ __forceinline__ void load_rows(const win_args& a, const win_span& s, 
 template <int HD>
 __device__ __forceinline__ void walk_partitions(const win_args& a, const win_span& s, const int32_t* __restrict__ bt, int j, int r0, int nn,
                                                 int c, int step, int lane) {
-    const int half = lane >> 5, l32 = lane & 31, G = a.hq / a.hkv, R = nn * G;
+    const int G = a.hq / a.hkv, R = nn * G;
     // its depth is below nn, so that from all_lo on every row sees every cached key
     const int all_lo = max(0, s.L + nn - a.window);
     // (of a draft with more nodes than the limits allow there are more tiles, and more partitions)
@@ -427,11 +427,10 @@ __device__ __forceinline__ void walk_partitions(const win_args& a, const win_spa
 // Small calls of at most 32 query rows per KV head (plain decoding): a wavefront per partition.
 template <int HD>
 __global__ __launch_bounds__(256, 2) void window_rows(win_args a) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = blockIdx.x % a.groups, pair = blockIdx.x / a.groups;
     const int j = pair % a.hkv, b = pair / a.hkv;
     const int r0 = a.row_off[b], nn = a.row_off[b + 1] - r0;
-    const int G = a.hq / a.hkv, R = nn * G;
     const win_span s = make_span(a.seq_len[b], nn, a);
     const int32_t* bt = a.block_table + (size_t)b * a.max_blocks;
     walk_partitions<HD>(a, s, bt, j, r0, nn, 4 * g + wave, 4 * a.groups, lane);
@@ -570,9 +569,7 @@ __device__ __forceinline__ void ring_keys(const win_args& a, const win_span& s, 
 #pragma unroll
                 for (int dt = 0; dt < NDT; dt++)
                     v.v[pp][dt] = *reinterpret_cast<const bf16x8*>(lds.ring + slot * T::BYTES + T::V + pp * T::PAGE + dt * 1024 + T::v_at(l32, half));
-            if (masked) {
-                odd |= __any(mask_values<HD>(v));
-            }
+            if (masked) odd |= __any(mask_values<HD>(v));
             bf16x8 pb[2];
             // (the matrix unit goes to the wavefront that has products for it, 113 -> 107 us for 8 x 512 tokens, 28 heads, 1024 keys)
             __builtin_amdgcn_s_setprio(1);
