@@ -646,14 +646,14 @@ __global__ __launch_bounds__(256) void window_merge(win_args a) {
     typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
     const int lane = threadIdx.x & 63, head = (blockIdx.y * 4 + (threadIdx.x >> 6)) * HEADS + lane / LANES;
     if ((blockIdx.y * 4 + (threadIdx.x >> 6)) * HEADS >= a.hq) return;
-    for (int row = blockIdx.x;; row += gridDim.x) {
+    for (int row = blockIdx.x; (size_t)row * a.hq < a.part_rows; row += gridDim.x) {
         const size_t prow = (size_t)row * a.hq + min(head, a.hq - 1);
         const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + prow;
         const _Float16* po = a.part_o + prow * HD + 8 * (lane % LANES);
         float2 x0[AHEAD];
         f16x8 v0[AHEAD];
         if constexpr (EARLY) {
-            // (in bounds whether the row and its partitions exist or not: the grid is no larger than the workspace's rows)
+            // (in bounds whether the row and its partitions exist or not: the loop goes no further than the workspace's rows)
 #pragma unroll
             for (int p = 0; p < AHEAD; p++) {
                 x0[p] = ml[min(p, a.max_parts - 1) * a.part_rows];
