@@ -55,7 +55,9 @@ struct win_span {
 __device__ __forceinline__ win_span make_span(int seq_len, int nn, const win_args& a) {
     const int cap = a.max_blocks * 16;
     win_span s;
-    s.L = min(seq_len - 1, cap);
+    // (A sequence may have outgrown its table: its windows lie where its positions are, and only the walk ends with the table.  The bound keeps
+    // sums with L in 32 bits: hs_create takes no more rows than 2^25.)
+    s.L = min(seq_len - 1, INT32_MAX - (1 << 25));
     s.total = min(s.L + nn, cap);
     s.first = max(0, s.L + 1 - a.window);
     s.sink_end = min(min(a.sinks, s.first), s.total);
