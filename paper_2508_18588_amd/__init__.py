@@ -116,8 +116,19 @@ class hs_prefill_args(C.Structure):
     _fields_ = [("chunk", C.c_int32), ("rows_hint", C.c_int32), ("kv_done", C.c_void_p)]
 
 
+def _fits_int32(name, value):
+    """value, which ctypes would cut to its lowest 32 bits without a word if it had more."""
+    if not -1 << 31 <= value < 1 << 31:
+        raise ValueError(f"{name}: {value} does not fit 32 bits")
+    return value
+
+
 class hs_window_args(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("layer", "window", "sinks", "chunk")] + [("q", C.c_void_p), ("out", C.c_void_p)]
+
+    def __init__(self, layer=0, window=0, sinks=0, chunk=0, q=None, out=None):
+        super().__init__(_fits_int32("layer", layer), _fits_int32("window", window), _fits_int32("sinks", sinks), _fits_int32("chunk", chunk),
+                         q, out)
 
 
 class hs_probs_args(C.Structure):
@@ -273,8 +284,8 @@ def hs_accept_commit(ctx, args: hs_accept_args, cache: hs_kv_cache, seq: hs_seq_
 
 def hs_set_window(ctx, window, sinks: int = 0):
     """window: one entry per layer (0 = the layer has none), or None to switch windows off."""
-    arr = None if window is None else (C.c_int32 * len(window))(*[int(x) for x in window])
-    _check(ctx, lib().hs_set_window(ctx, arr, int(sinks)))
+    arr = None if window is None else (C.c_int32 * len(window))(*[_fits_int32("window", int(x)) for x in window])
+    _check(ctx, lib().hs_set_window(ctx, arr, _fits_int32("sinks", int(sinks))))
 
 
 def hs_attention_window(ctx, cache: hs_kv_cache, seq: hs_seq_state, step: hs_step, args: hs_window_args, stream=None):
