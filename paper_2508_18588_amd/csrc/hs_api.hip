@@ -255,7 +255,12 @@ hs_status hs_set_window(hs_ctx* ctx, const int32_t* window, int32_t sinks) {
     if (sinks < 0 || sinks > HS_WINDOW_MAX) return fail(ctx, HS_ERR_INVALID_ARG, "hs_set_window: sinks");
     for (int l = 0; l < ctx->desc.n_layers; l++)
         if (window[l] < 0 || window[l] > HS_WINDOW_MAX) return fail(ctx, HS_ERR_INVALID_ARG, "hs_set_window: window");
-    ctx->window.assign(window, window + ctx->desc.n_layers);
+    try {
+        std::vector<int32_t> copy(window, window + ctx->desc.n_layers);
+        ctx->window.swap(copy);
+    } catch (const std::bad_alloc&) {      // (what was set before stays)
+        return fail(ctx, HS_ERR_CAPACITY, "hs_set_window: no memory for the windows");
+    }
     ctx->sinks = sinks;
     return HS_OK;
 }
