@@ -1,9 +1,12 @@
 """Paths of the window attention and of the probabilities that take certain sizes: infinities and NaNs where a draft's keys come in partitions
-or whole for a large batch, chunks whose keys come in several runs, and fewer long rows of logits than compute units."""
+or whole for a large batch and in the plain kernel, chunks whose keys come in several runs, fewer long rows of logits than compute units, the
+largest vocabularies, and more sequences than the device has places for."""
 import numpy as np
 import pytest
 import torch
 
+from paper_2508_18588_amd import HS_FLAG_REFERENCE_KERNELS, hs_set_flags
+from test_gpu_probs import check as check_accept, distributions, drafted, uniforms
 from window_common import bound, chain, engine, lay_out, lay_out_chunk, queries, random_tree, reference, visible
 
 pytestmark = pytest.mark.gpu
@@ -151,4 +154,54 @@ def test_fewer_long_rows_than_compute_units(vocab, rows):
         assert ((out[r].double() - want).abs() <= tol + 2.0 ** -125).all()
     eng.probs(x[3:5], few, 0.8)
     assert torch.equal(few, out[3:5])
+    eng.close()
+
+
+def test_a_vocabulary_beyond_25_million():
+    """More slices of sums than 48 KB of LDS hold, where sums are the last launch's own: two rejected children behind one launch of sums."""
+    vocab, m = 26000003, 4
+    eng = engine(1, 1, 64, [8], m, vocab=vocab)
+    x = torch.randn(m, vocab, device="cuda:0")
+    p, q = torch.empty_like(x), torch.empty_like(x)
+    eng.probs(x * 9, p, 1.1)
+    eng.probs(x * 8 + torch.randn(m, vocab, device="cuda:0"), q, 1.0)
+    y = x[0].double() * 9
+    want = torch.softmax((x[0] * 9).double() / float(np.float32(1.1)), -1)
+    # (as for fewer long rows, with 25391 units: 397 one after the other)
+    tol = want * 2.0 ** -24 * (450 + 2 * ((y.amax() - y) / 1.1).clamp(max=200))
+    assert ((p[0].double() - want).abs() <= tol + 2.0 ** -125).all()
+    par = np.asarray([-1, 0, 0, 0])
+    toks = [np.asarray([0] + [int(t) for t in q[0].topk(3).indices], np.int32)]
+    for accept in (0.0, 1.0 - 2.0 ** -24):
+        for sample in (0.0, 0.3, 0.9999, 1.0 - 2.0 ** -24):
+            for d in (q, None):
+                check_accept(eng, [par], toks, p, d, np.full(m, accept), np.full(1, sample))
+    eng.close()
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+def test_more_sequences_than_workgroups_that_sum(drawn):
+    rng, vocab, n = np.random.default_rng(8), 300, 1500
+    eng = engine(1, 1, 64, [8] * n, 4, vocab=vocab)
+    pars = [None if b % 5 == 2 else chain(int(rng.integers(0, 4))) for b in range(n)]
+    m = sum(len(x) for x in pars if x is not None)
+    p, q = distributions(m, vocab, 3.0, 0.7, torch.float32, 9)
+    toks = drafted(pars, q if drawn else p, vocab, rng)
+    got = check_accept(eng, pars, toks, p, q if drawn else None, uniforms(rng, m), uniforms(rng, n))
+    assert got["accept_len"].sum() > 0
+    eng.close()
+
+
+def test_the_plain_kernel_on_a_cache_of_16_bits():
+    rng = np.random.default_rng(9)
+    lens, pars = [1, 70, 300], [chain(0), random_tree(9, rng), chain(5)]
+    eng = engine(8, 2, 64, lens, 9)
+    m = lay_out(eng, lens, pars)
+    q = queries(m, eng)
+    hs_set_flags(eng.ctx, HS_FLAG_REFERENCE_KERNELS)
+    eng._bind_workspace()
+    for window, sinks in ((1, 0), (4, 2), (50, 4), (1000, 0)):
+        agree(*_case(eng, m, lens, pars, q, window, sinks, []))
+    L = lens[2] - 1
+    agree(*_case(eng, m, lens, pars, q, 50, 4, [(2, L + 1 - 50, 0, 3, INF), (2, L - 50, 1, 4, NAN), (2, L + 2, 1, 5, NAN), (1, 69 + 9, 0, 6, NAN)]))
     eng.close()
