@@ -263,7 +263,8 @@ hs_status hs_draft_group(hs_ctx* ctx, const hs_group_draft_args* args, const hs_
 
 /* Sliding-window attention with sinks, per layer: window is a HOST array of n_layers entries (copied); in a layer with
  * window[l] >= 1 a row at position p sees, of what it sees otherwise, the positions t > p - window[l] and the first
- * `sinks` ones, t < sinks; 0 leaves the layer as it is.  NULL: no layer has a window.  hs_verify (with every flag) and
+ * `sinks` ones, t < sinks; 0 leaves the layer as it is.  NULL: no layer has a window.  (HS_ERR_CAPACITY: the host has no memory
+ * for the copy; the windows stay as they were.)  hs_verify (with every flag) and
  * hs_prefill follow it from the next call on; what a HIP graph has recorded keeps the windows of its recording.  A row's
  * result does not depend on what other rows its sequence has, nor on how a text is cut into chunks, as without windows.
  * Only pages that hold a position some row of the call sees are looked up and read: where all layers have windows, a page

@@ -502,8 +502,9 @@ __global__ __launch_bounds__(256) void verify_pick(verify_args a) {
 }
 
 // Logits that fit into the last cache are read a second time from there by a launch of their own; of more, a workgroup per row reads its row
-// twice while the cache has it, in full rounds of a row per compute unit; the rest again by two launches (1088 rows of 152064 tokens: the rest in a
-// round of rows cost 357 against 346 us; everything by such pairs of launches, 192 MB of logits at a time, 343 against 315).
+// twice while the cache has it, in full rounds of a row per compute unit; the rest again by two launches if it fits into the cache, otherwise by a
+// round of rows too, which leaves compute units without one (1088 rows of 152064 tokens: the rest in a round of rows cost 357 against 346 us;
+// everything by such pairs of launches, 192 MB of logits at a time, 343 against 315).
 template <typename TI, typename TO>
 void launch_rows(const hs_ctx* ctx, const probs_args& all, hipStream_t st) {
     auto pairs = [&](int from, int rows) {

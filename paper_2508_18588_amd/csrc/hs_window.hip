@@ -5,7 +5,7 @@
 //   out[row, h] = sum_t softmax_t(q[row, h] . k[t, h / G] / sqrt(head_dim)) v[t, h / G]  over the visible t; 0 if there is none
 //
 // A sequence of L cached tokens and nn rows needs the keys [0, sinks) and [L + 1 - window, L + nn), whatever its length: only
-// their pages are looked up and read.
+// their pages are looked up and read.  (Of a sequence that has outgrown its block table, what of these lies in the table.)
 //
 // Scores are computed transposed, S^T = K . Q^T (v_mfma_f32_32x32x16_bf16), for 32 query rows (rows of one token's G query heads, which share a
 // KV head, are neighbours) and 32 keys at a time, so that a lane has the scores of one query row and the softmax statistics are its own scalars.
@@ -15,10 +15,10 @@
 //
 // A draft's rows are few and its keys many, and memory bounds it.  Four row tiles share a stream of key tiles through LDS; a workgroup walks all
 // keys of a (sequence, KV head), or a run of partitions, whose results a launch of its own joins (see plan_rows).  128 single tokens, 28 heads,
-// 1024 keys: 51 us, 5.3 TB/s (a copy reaches 4.9); 256 drafts, 4096 keys: 360 us, 5.2 TB/s; 64 trees of 17 nodes, 40 heads, 2048 keys: 97 us, 5.8
+// 1024 keys: 51 us, 5.3 TB/s (a copy reaches 4.9); 256 drafts, 4096 keys: 362 us, 5.2 TB/s; 64 trees of 17 nodes, 40 heads, 2048 keys: 97 us, 5.8
 // TB/s; the stream alone, without products, 319 and 95 us when these took 412 and 131.  A chunk's rows are many: a workgroup takes 128 of them
-// through all their keys (8 x 512 tokens, 28 heads, 1024 keys: 94 us, 640 TFLOP/s of the 1215 that a large product of matrices reaches; matrix unit,
-// vector unit and LDS are each busy for two fifths of the time, with two wavefronts per SIMD to overlap them).
+// through all their keys (512 tokens each of 7 sequences and 257 of an eighth, 28 heads, 1024 keys: 89 us, 637 TFLOP/s of the 1215 that a large product
+// of matrices reaches; matrix unit, vector unit and LDS are each busy for two fifths of the time, with two wavefronts per SIMD to overlap them).
 //
 // Every sum has an order that depends on absolute key positions only (32-key tiles, partitions of part_keys, if any, merged in index order;
 // keys that a row does not see contribute exact zeros): a row's result does not depend on what other rows are computed with it.
