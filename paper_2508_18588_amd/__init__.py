@@ -18,13 +18,14 @@ _CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libhistospec.so")
 
 HS_OK, HS_ERR_INVALID_ARG, HS_ERR_CAPACITY, HS_ERR_UNSUPPORTED, HS_ERR_HIP = 0, -1, -2, -3, -4
-HS_DEV_BLOCK_TABLE_OVERFLOW, HS_DEV_POSITION_OVERFLOW, HS_DEV_ROW_OVERFLOW = 1, 2, 4
+HS_DEV_BLOCK_TABLE_OVERFLOW, HS_DEV_POSITION_OVERFLOW, HS_DEV_ROW_OVERFLOW, HS_DEV_PAGES_EXHAUSTED, HS_DEV_PAGE_REFUSED = 1, 2, 4, 8, 16
 HS_K_FIXED, HS_K_MATCHLEN, HS_K_AIMD = 0, 1, 2
 HS_ACCEPT_GREEDY, HS_ACCEPT_REJECTION = 0, 1
 HS_FLAG_REFERENCE_KERNELS, HS_FLAG_FP32_ACTIVATIONS, HS_FLAG_WORKSPACE_LOGITS = 1, 2, 4
 HS_GATE_WORDS, HS_GATE_TABLE = 32, 8
 HS_F32, HS_BF16 = 0, 1
 HS_WINDOW_MAX = 1 << 30
+HS_PAGES_MAX, HS_LOGPROBS_TOP = 1 << 22, 32
 
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -142,6 +143,31 @@ class hs_accept_probs_args(C.Structure):
                 ("u_accept", C.c_void_p), ("u_sample", C.c_void_p)]
 
 
+class hs_shared_prefix(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_groups", "max_members", "max_prefix")] + [("group_off", C.c_void_p), ("prefix_len", C.c_void_p)]
+
+    def __init__(self, n_groups=0, max_members=0, max_prefix=0, group_off=None, prefix_len=None):
+        super().__init__(_fits_int32("n_groups", n_groups), _fits_int32("max_members", max_members), _fits_int32("max_prefix", max_prefix),
+                         group_off, prefix_len)
+
+
+class hs_shared_args(C.Structure):
+    _fields_ = [("layer", C.c_int32), ("prefix", hs_shared_prefix), ("q", C.c_void_p), ("out", C.c_void_p)]
+
+    def __init__(self, layer=0, prefix=None, q=None, out=None):
+        super().__init__(_fits_int32("layer", layer), hs_shared_prefix() if prefix is None else prefix, q, out)
+
+
+class hs_page_pool(C.Structure):
+    _fields_ = [("refs", C.c_void_p), ("table", C.c_void_p), ("scratch", C.c_void_p)]
+
+
+class hs_logprobs_args(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("logits_stride", C.c_int64), ("logits_type", C.c_int32), ("rows", C.c_int32), ("n", C.c_int32),
+                ("emitted", C.c_int32), ("temperature", C.c_float), ("top", C.c_int32), ("row", C.c_void_p), ("token", C.c_void_p),
+                ("live", C.c_void_p), ("logprob", C.c_void_p), ("entropy", C.c_void_p), ("top_token", C.c_void_p), ("top_logprob", C.c_void_p)]
+
+
 HS_PREFILL_CHUNK_MAX = 1024
 
 
@@ -149,7 +175,8 @@ EXPORTS = ("hs_create", "hs_destroy", "hs_last_error", "hs_set_flags", "hs_works
            "hs_draft", "hs_draft_group", "hs_verify", "hs_accept", "hs_kv_commit", "hs_poll_error", "hs_debug_buffer",
            "hs_set_profile", "hs_get_profile", "hs_debug_gemm", "hs_gate_table_build", "hs_prefill", "hs_plan_allocation",
            "hs_debug_capture", "hs_debug_capture_bytes", "hs_debug_philox", "hs_draft_static", "hs_accept_commit", "hs_debug_rowmax_groups",
-           "hs_set_window", "hs_attention_window", "hs_probs", "hs_accept_probs")
+           "hs_set_window", "hs_attention_window", "hs_probs", "hs_accept_probs", "hs_set_shared_prefix", "hs_attention_shared",
+           "hs_logprobs", "hs_pages_scratch_bytes", "hs_pages_free", "hs_pages_fork", "hs_pages_reserve", "hs_pages_compact")
 
 _lib = None
 
@@ -193,6 +220,17 @@ def lib():
                                           C.POINTER(hs_window_args), vp]
         L.hs_probs.argtypes = [vp, C.POINTER(hs_probs_args), vp]
         L.hs_accept_probs.argtypes = [vp, C.POINTER(hs_accept_probs_args), C.POINTER(hs_seq_state), C.POINTER(hs_step), vp]
+        L.hs_set_shared_prefix.argtypes = [vp, C.POINTER(hs_shared_prefix)]
+        L.hs_attention_shared.argtypes = [vp, C.POINTER(hs_kv_cache), C.POINTER(hs_seq_state), C.POINTER(hs_step),
+                                          C.POINTER(hs_shared_args), vp]
+        L.hs_logprobs.argtypes = [vp, C.POINTER(hs_logprobs_args), C.POINTER(hs_seq_state), C.POINTER(hs_step), vp]
+        L.hs_pages_scratch_bytes.argtypes = [vp, C.c_int32]
+        L.hs_pages_scratch_bytes.restype = C.c_size_t
+        pool = [vp, C.POINTER(hs_kv_cache), C.POINTER(hs_seq_state), C.POINTER(hs_page_pool)]
+        L.hs_pages_free.argtypes = pool + [vp, vp, vp]
+        L.hs_pages_fork.argtypes = pool + [vp, vp]
+        L.hs_pages_reserve.argtypes = pool + [vp, C.c_int32, vp]
+        L.hs_pages_compact.argtypes = [vp, C.POINTER(hs_kv_cache), C.POINTER(hs_page_pool), vp, vp, vp]
         L.hs_poll_error.argtypes = [vp, vp, C.POINTER(C.c_uint32)]
         L.hs_debug_buffer.argtypes = [vp, C.c_int32, C.POINTER(vp), C.POINTER(C.c_size_t)]
         L.hs_debug_capture_bytes.argtypes = [vp]
@@ -298,6 +336,38 @@ def hs_probs(ctx, args: hs_probs_args, stream=None):
 
 def hs_accept_probs(ctx, args: hs_accept_probs_args, seq: hs_seq_state, step: hs_step, stream=None):
     _check(ctx, lib().hs_accept_probs(ctx, C.byref(args), C.byref(seq), C.byref(step), stream))
+
+
+def hs_set_shared_prefix(ctx, prefix: hs_shared_prefix | None):
+    _check(ctx, lib().hs_set_shared_prefix(ctx, None if prefix is None else C.byref(prefix)))
+
+
+def hs_attention_shared(ctx, cache: hs_kv_cache, seq: hs_seq_state, step: hs_step, args: hs_shared_args, stream=None):
+    _check(ctx, lib().hs_attention_shared(ctx, C.byref(cache), C.byref(seq), C.byref(step), C.byref(args), stream))
+
+
+def hs_logprobs(ctx, args: hs_logprobs_args, seq: hs_seq_state | None = None, step: hs_step | None = None, stream=None):
+    _check(ctx, lib().hs_logprobs(ctx, C.byref(args), None if seq is None else C.byref(seq), None if step is None else C.byref(step), stream))
+
+
+def hs_pages_scratch_bytes(ctx, n_blocks: int) -> int:
+    return lib().hs_pages_scratch_bytes(ctx, _fits_int32("n_blocks", n_blocks))
+
+
+def hs_pages_free(ctx, cache: hs_kv_cache, seq: hs_seq_state, pool: hs_page_pool, first: int, end: int, stream=None):
+    _check(ctx, lib().hs_pages_free(ctx, C.byref(cache), C.byref(seq), C.byref(pool), first, end, stream))
+
+
+def hs_pages_fork(ctx, cache: hs_kv_cache, seq: hs_seq_state, pool: hs_page_pool, parent: int, stream=None):
+    _check(ctx, lib().hs_pages_fork(ctx, C.byref(cache), C.byref(seq), C.byref(pool), parent, stream))
+
+
+def hs_pages_reserve(ctx, cache: hs_kv_cache, seq: hs_seq_state, pool: hs_page_pool, extra: int, first: int | None = None, stream=None):
+    _check(ctx, lib().hs_pages_reserve(ctx, C.byref(cache), C.byref(seq), C.byref(pool), first, _fits_int32("extra", extra), stream))
+
+
+def hs_pages_compact(ctx, cache: hs_kv_cache, pool: hs_page_pool, n_live: int | None = None, moved: int | None = None, stream=None):
+    _check(ctx, lib().hs_pages_compact(ctx, C.byref(cache), C.byref(pool), n_live, moved, stream))
 
 
 def hs_poll_error(ctx, stream=None) -> int:

@@ -61,6 +61,8 @@ void layout_workspace(hs_ctx* ctx) {
     w.probs_sums = take((size_t)HS_PROBS_ROUNDS * l.max_batch * hs_probs_slices(d.vocab) * sizeof(double));
     w.probs_records = take((size_t)HS_PROBS_ROUNDS * l.max_batch * HS_PROBS_RECORD);
     w.probs_stats = take(HS_PROBS_STATS * 8);
+    w.logprobs = take(hs_logprobs_scratch(d.vocab));
+    w.shared_parts = take((size_t)l.max_batch * 4);
     w.total = off;
 }
 
@@ -119,6 +121,33 @@ bool type_ok(int type) { return type == HS_F32 || type == HS_BF16; }
 // rows over the vocabulary: their stride, and their elements' own alignment
 bool rows_ok(const hs_ctx* ctx, const void* p, long long stride, int type) {
     return stride >= ctx->desc.vocab && ((uintptr_t)p & (type == HS_F32 ? 3u : 1u)) == 0;
+}
+
+bool prefix_ok(const hs_ctx* ctx, const hs_shared_prefix* p) {
+    return p->n_groups >= 1 && p->n_groups <= ctx->lim.max_batch && p->max_members >= 1 && p->max_members <= ctx->lim.max_batch &&
+           p->max_prefix >= 0 && p->group_off && p->prefix_len;
+}
+
+// What the calls on pages have in common.
+hs_status pages_ok(hs_ctx* ctx, const char* who, const hs_kv_cache* cache, const hs_page_pool* pool) {
+    auto bad = [&](hs_status code, const char* what) {
+        ctx->err = std::string(who) + ": " + what;
+        return code;
+    };
+    if (!ctx->ws) return bad(HS_ERR_CAPACITY, "no workspace bound");
+    if (!cache_ok(cache) || (((uintptr_t)cache->k | (uintptr_t)cache->v) & 15u) != 0) return bad(HS_ERR_INVALID_ARG, "cache");
+    if (cache->n_blocks > HS_PAGES_MAX) return bad(HS_ERR_UNSUPPORTED, "more than HS_PAGES_MAX pages");
+    if (!pool || !pool->refs || !pool->table || !pool->scratch || ((uintptr_t)pool->scratch & 15u) != 0)
+        return bad(HS_ERR_INVALID_ARG, "page pool");
+    return HS_OK;
+}
+hs_status pages_ok(hs_ctx* ctx, const char* who, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_page_pool* pool) {
+    if (const hs_status s = pages_ok(ctx, who, cache, pool); s != HS_OK) return s;
+    if (!seq_ok(ctx, seq) || seq->block_table != pool->table) {
+        ctx->err = std::string(who) + ": sequence state, or a block table that is not the pool's";
+        return HS_ERR_INVALID_ARG;
+    }
+    return HS_OK;
 }
 
 }  // namespace
@@ -265,6 +294,17 @@ hs_status hs_set_window(hs_ctx* ctx, const int32_t* window, int32_t sinks) {
     return HS_OK;
 }
 
+hs_status hs_set_shared_prefix(hs_ctx* ctx, const hs_shared_prefix* prefix) {
+    if (!ctx) return HS_ERR_INVALID_ARG;
+    if (!prefix) {
+        ctx->shared = {};
+        return HS_OK;
+    }
+    if (!prefix_ok(ctx, prefix)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_set_shared_prefix: groups, hints or null arrays");
+    ctx->shared = *prefix;
+    return HS_OK;
+}
+
 size_t hs_workspace_bytes(const hs_ctx* ctx) { return ctx ? ctx->lay.total : 0; }
 
 hs_status hs_bind_workspace(hs_ctx* ctx, void* dev_ptr, size_t bytes) {
@@ -387,12 +427,15 @@ hs_status hs_verify(hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* s
         pr.end();
         const int window = hs_window_of(ctx, l);
         const bool windowed = window > 0 && !hs_plain_kernels(ctx);
+        const bool shares = window == 0 && ctx->shared.n_groups > 0 && !hs_plain_kernels(ctx);
         pr.begin(0, l % 4 == 0);
         if (windowed) hs_launch_window_attention(ctx, l, cache, seq, step, q, attn, window, ctx->sinks, st);
+        else if (shares) hs_launch_shared_attention(ctx, l, cache, seq, step, &ctx->shared, q, attn, st);
         else hs_launch_attention(ctx, l, cache, seq, step, q, attn, st, window, ctx->sinks);
         pr.end();
         pr.begin(3);
         if (windowed) hs_launch_window_merge(ctx, cache, seq, step, attn, window, ctx->sinks, st);
+        else if (shares) hs_launch_shared_merge(ctx, cache, seq, step, &ctx->shared, attn, st);
         else hs_launch_attention_merge(ctx, seq, step, attn, expected, st);
         pr.end();
         pr.begin(1);
@@ -624,6 +667,116 @@ hs_status hs_attention_window(hs_ctx* ctx, const hs_kv_cache* cache, const hs_se
         }
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail_hip(ctx, "hs_attention_window", e);
+    return HS_OK;
+}
+
+hs_status hs_attention_shared(hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step,
+                              const hs_shared_args* args, hs_stream stream) {
+    if (!ctx) return HS_ERR_INVALID_ARG;
+    if (!ctx->ws) return fail(ctx, HS_ERR_CAPACITY, "no workspace bound");
+    if (!cache_ok(cache)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_shared: cache");
+    if (!seq_ok(ctx, seq)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_shared: sequence state");
+    if (!args || !args->q || !args->out) return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_shared: null queries or output");
+    if ((((uintptr_t)args->q | (uintptr_t)args->out) & 15u) != 0)
+        return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_shared: queries and output must be 16-byte aligned");
+    if (args->layer < 0 || args->layer >= ctx->desc.n_layers) return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_shared: layer");
+    if (!prefix_ok(ctx, &args->prefix)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_shared: groups, hints or null arrays");
+    if (!step || !step->row_off || !step->pos || !step->anc_mask || !step->row2seq)
+        return fail(ctx, HS_ERR_INVALID_ARG, "hs_attention_shared: step arrays");
+    const hipStream_t st = (hipStream_t)stream;
+    (void)hipGetLastError();
+    if (hs_plain_kernels(ctx)) {      // (every sequence reads its own table: the same result)
+        hs_launch_attention(ctx, args->layer, cache, seq, step, args->q, args->out, st);
+    } else {
+        hs_launch_shared_attention(ctx, args->layer, cache, seq, step, &args->prefix, args->q, args->out, st);
+        hs_launch_shared_merge(ctx, cache, seq, step, &args->prefix, args->out, st);
+    }
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail_hip(ctx, "hs_attention_shared", e);
+    return HS_OK;
+}
+
+hs_status hs_logprobs(hs_ctx* ctx, const hs_logprobs_args* args, const hs_seq_state* seq, const hs_step* step, hs_stream stream) {
+    if (!ctx) return HS_ERR_INVALID_ARG;
+    if (!ctx->ws) return fail(ctx, HS_ERR_CAPACITY, "no workspace bound");
+    if (!args || !args->logprob) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: null output");
+    if (!(args->temperature >= 1e-30f && args->temperature <= 1e30f))
+        return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: temperature must be positive and finite (1e-30 to 1e30)");
+    if (args->top < 0 || args->top > HS_LOGPROBS_TOP || args->top > ctx->desc.vocab)
+        return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: top");
+    if (args->top > 0 && (!args->top_token || !args->top_logprob)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: null alternatives");
+    const void* logits = args->logits;
+    long long stride = args->logits_stride;
+    int type = args->logits_type, rows = args->rows;
+    if (args->emitted) {
+        if (!seq_ok(ctx, seq)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: sequence state");
+        if (!step || !step->row_off || !step->n_out || !step->out_tok || !step->path_row)
+            return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: step arrays");
+        if (!logits) {
+            if (hs_head_fused(ctx, step))
+                return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: no logits are kept: pass hs_step.logits or set HS_FLAG_WORKSPACE_LOGITS");
+            logits = step->logits ? (const void*)step->logits : (const void*)(ctx->ws + ctx->lay.logits);
+            stride = ctx->desc.vocab;
+            type = HS_F32;
+            rows = ctx->lim.max_rows;
+        }
+    } else {
+        if (!logits) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: null logits");
+        if (args->n < 0) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: n");
+        if (args->n > 0 && !args->token) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: null tokens");
+    }
+    if (!type_ok(type)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: type");
+    if (rows < 0) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: rows");
+    if (!rows_ok(ctx, logits, stride, type)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: stride below the vocabulary, or misaligned rows");
+    if (!args->emitted && args->n == 0) return HS_OK;
+    (void)hipGetLastError();
+    hs_launch_logprobs(ctx, args, seq, step, logits, stride, type, rows, (hipStream_t)stream);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail_hip(ctx, "hs_logprobs", e);
+    return HS_OK;
+}
+
+size_t hs_pages_scratch_bytes(const hs_ctx* ctx, int32_t n_blocks) {
+    return ctx && n_blocks >= 1 && n_blocks <= HS_PAGES_MAX ? hs_pages_scratch(ctx, n_blocks) : 0;
+}
+
+hs_status hs_pages_free(hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_page_pool* pool, const int32_t* from,
+                        const int32_t* to, hs_stream stream) {
+    if (!ctx) return HS_ERR_INVALID_ARG;
+    if (const hs_status s = pages_ok(ctx, "hs_pages_free", cache, seq, pool); s != HS_OK) return s;
+    if (!from || !to) return fail(ctx, HS_ERR_INVALID_ARG, "hs_pages_free: null positions");
+    (void)hipGetLastError();
+    hs_launch_pages_free(ctx, cache, seq, pool, from, to, (hipStream_t)stream);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail_hip(ctx, "hs_pages_free", e);
+    return HS_OK;
+}
+
+hs_status hs_pages_fork(hs_ctx* ctx, const hs_kv_cache* cache, hs_seq_state* seq, const hs_page_pool* pool, const int32_t* parent,
+                        hs_stream stream) {
+    if (!ctx) return HS_ERR_INVALID_ARG;
+    if (const hs_status s = pages_ok(ctx, "hs_pages_fork", cache, seq, pool); s != HS_OK) return s;
+    if (!parent) return fail(ctx, HS_ERR_INVALID_ARG, "hs_pages_fork: null parents");
+    (void)hipGetLastError();
+    hs_launch_pages_fork(ctx, cache, seq, pool, parent, (hipStream_t)stream);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail_hip(ctx, "hs_pages_fork", e);
+    return HS_OK;
+}
+
+hs_status hs_pages_reserve(hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_page_pool* pool, const int32_t* from,
+                           int32_t extra, hs_stream stream) {
+    if (!ctx) return HS_ERR_INVALID_ARG;
+    if (const hs_status s = pages_ok(ctx, "hs_pages_reserve", cache, seq, pool); s != HS_OK) return s;
+    if (extra < 0) return fail(ctx, HS_ERR_INVALID_ARG, "hs_pages_reserve: extra");
+    (void)hipGetLastError();
+    hs_launch_pages_reserve(ctx, cache, seq, pool, from, extra, (hipStream_t)stream);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail_hip(ctx, "hs_pages_reserve", e);
+    return HS_OK;
+}
+
+hs_status hs_pages_compact(hs_ctx* ctx, const hs_kv_cache* cache, const hs_page_pool* pool, int32_t* n_live, int32_t* moved, hs_stream stream) {
+    if (!ctx) return HS_ERR_INVALID_ARG;
+    if (const hs_status s = pages_ok(ctx, "hs_pages_compact", cache, pool); s != HS_OK) return s;
+    (void)hipGetLastError();
+    hs_launch_pages_compact(ctx, cache, pool, n_live, moved, (hipStream_t)stream);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail_hip(ctx, "hs_pages_compact", e);
     return HS_OK;
 }
 

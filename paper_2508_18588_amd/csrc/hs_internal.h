@@ -34,7 +34,7 @@ constexpr size_t HS_PROBS_CACHED = 192u << 20, HS_PROBS_STATS = 262144;
 static inline int hs_probs_slices(int vocab) { return (vocab + HS_PROBS_SLICE - 1) / HS_PROBS_SLICE; }
 
 struct hs_workspace_layout {
-    size_t x, xn, qkv, q, attn, act, part_o, part_ml, logits, logits_bytes, rowmax, draft_best, gemm_part, gemm_part_bytes, err, pf_len, row_info, att_work, att_list, reject_stats, reject_walk, probs_sums, probs_records, probs_stats, total;
+    size_t x, xn, qkv, q, attn, act, part_o, part_ml, logits, logits_bytes, rowmax, draft_best, gemm_part, gemm_part_bytes, err, pf_len, row_info, att_work, att_list, reject_stats, reject_walk, probs_sums, probs_records, probs_stats, logprobs, shared_parts, total;
 };
 
 struct hs_ctx {
@@ -47,6 +47,7 @@ struct hs_ctx {
     uint32_t flags = 0;
     std::vector<int32_t> window;   // hs_set_window: per layer, 0 = none; empty: no layer has one
     int32_t sinks = 0;
+    hs_shared_prefix shared = {};  // hs_set_shared_prefix; no groups: none
     char* capture = nullptr;  // hs_debug_capture: snapshots of the last layer's projection inputs
     char* ws = nullptr;
     size_t ws_bytes = 0;
@@ -239,3 +240,21 @@ void hs_launch_accept_commit(const hs_ctx* ctx, const hs_accept_args* args, cons
 void hs_launch_probs(const hs_ctx* ctx, const hs_probs_args* args, hipStream_t st);
 void hs_launch_accept_probs(const hs_ctx* ctx, const hs_accept_probs_args* args, const hs_seq_state* seq, const hs_step* step,
                             hipStream_t st);
+// Log probabilities (hs_logprobs.hip), of `rows` rows of logits; the bytes of the workspace that they need.
+size_t hs_logprobs_scratch(int vocab);
+void hs_launch_logprobs(const hs_ctx* ctx, const hs_logprobs_args* args, const hs_seq_state* seq, const hs_step* step, const void* logits,
+                        long long stride, int type, int rows, hipStream_t st);
+// Attention of sequences that share prefixes (hs_shared.hip): partial results, and the launch that joins them.
+void hs_launch_shared_attention(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step,
+                                const hs_shared_prefix* pre, const void* q, void* out, hipStream_t st);
+void hs_launch_shared_merge(const hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step, const hs_shared_prefix* pre,
+                            void* out, hipStream_t st);
+// The pages of the cache (hs_pages.hip).
+size_t hs_pages_scratch(const hs_ctx* ctx, int n_blocks);
+void hs_launch_pages_free(const hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_page_pool* pool, const int32_t* from,
+                          const int32_t* to, hipStream_t st);
+void hs_launch_pages_fork(const hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_page_pool* pool, const int32_t* parent,
+                          hipStream_t st);
+void hs_launch_pages_reserve(const hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_page_pool* pool, const int32_t* from, int extra,
+                             hipStream_t st);
+void hs_launch_pages_compact(const hs_ctx* ctx, const hs_kv_cache* cache, const hs_page_pool* pool, int32_t* n_live, int32_t* moved, hipStream_t st);

@@ -1,0 +1,313 @@
+// Log probabilities of tokens, the entropy of their distributions, and the largest alternatives.  With x_t = (l_t - max l) / T and S = sum exp(x):
+//
+//   log p(t) = x_t - ln S        H = ln S - sum(x exp(x)) / S        the k largest l_t, the lower token first among equal ones
+//
+// Bound by memory: the logits are read once.  The first launch takes a vocabulary in chunks of 8192 tokens, a workgroup each, and leaves each chunk's
+// maximum, sum of exp and sum of x exp, and the largest logit of every unit of 256 tokens; the second joins the chunks in their order, in 64 bits.
+// A row's k largest tokens lie in the k units with the largest maxima (the lower unit first among equal ones): k units are in front of any
+// other one, each with a token that is in front of all of its tokens.  So the second launch reads k units again and nothing else.
+// Chunks and units belong to the vocabulary alone: a row's results have the same bits whatever else is asked.
+#include <algorithm>
+#include <cmath>
+
+#include "hs_internal.h"
+#include "hs_lanes.h"
+
+namespace {
+
+constexpr int CHUNK = 8192, UNIT = 256, CHUNK_UNITS = CHUNK / UNIT;
+constexpr int UNITS_LDS = 2048;      // a row's units in LDS; of larger vocabularies (from 524288 tokens on) they are read again from memory
+
+struct lp_stat { float m, s, e, unused; };      // largest logit; sums of w and w d, w = exp2(d), d = (l - m) log2(e) / T
+struct lp_args {
+    const void* logits;
+    size_t stride;
+    int rows, vocab, n, first, top, chunks, units;      // first: the number of entry 0 of this launch
+    float c, inv_t;                                     // log2(e) / T
+    double t;
+    const int32_t *row, *token, *live;
+    // emitted tokens: entry (b, i) = the i-th one of sequence b
+    const int32_t *row_off, *n_out, *out_tok, *path_row;
+    int k_stride, batch;
+    lp_stat* stats;          // [entries of the launch][chunks]
+    float* most;             // [entries of the launch][units]
+    float *logprob, *entropy, *top_logprob;
+    int32_t* top_token;
+};
+
+// An entry's row and token.  Row -1: nothing is asked; -2: there is no such row.
+struct lp_entry { int row, token; };
+__device__ __forceinline__ lp_entry entry_of(const lp_args& a, int i) {
+    lp_entry e = {-1, -1};
+    if (a.row_off) {
+        const int b = i / a.k_stride, at = i % a.k_stride;
+        if (b >= a.batch || at >= a.n_out[b]) return e;
+        e.row = a.row_off[b] + a.path_row[i];
+        e.token = a.out_tok[i];
+    } else {
+        if (a.live && i >= *a.live) return e;
+        e.row = a.row ? a.row[i] : i;
+        e.token = a.token[i];
+    }
+    if ((unsigned)e.row >= (unsigned)a.rows) e.row = -2;
+    return e;
+}
+
+__device__ __forceinline__ float wide(float v) { return v; }
+__device__ __forceinline__ float wide(bf16_t v) { return bf16_to_f32(v); }
+template <typename T> constexpr int run_of = 16 / sizeof(T);
+// A run of 16 bytes that begins at token i; tokens beyond the vocabulary: -inf.
+template <typename T>
+__device__ __forceinline__ void load_run(const T* __restrict__ row, int i, int vocab, bool aligned, float (&v)[run_of<T>]) {
+    constexpr int RUN = run_of<T>;
+    if (aligned && i + RUN <= vocab) {
+        typedef T run_t __attribute__((ext_vector_type(RUN)));
+        const run_t x = __builtin_nontemporal_load(reinterpret_cast<const run_t*>(row + i));
+#pragma unroll
+        for (int e = 0; e < RUN; e++) v[e] = wide((T)x[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < RUN; e++) v[e] = i + e < vocab ? wide(row[i + e]) : -INFINITY;
+    }
+}
+__device__ __forceinline__ float wave_sum_f32(float v) {
+    auto step = [&](unsigned other) { v += __uint_as_float(other); };
+    step(lane_xor<32>(__float_as_uint(v)));
+    step(lane_xor<16>(__float_as_uint(v)));
+    step(lane_xor<8>(__float_as_uint(v)));
+    step(lane_xor<4>(__float_as_uint(v)));
+    step(lane_xor<2>(__float_as_uint(v)));
+    step(lane_xor<1>(__float_as_uint(v)));
+    return v;
+}
+
+// A chunk: every lane has 32 of its tokens, in runs of 16 bytes, a wavefront's side by side: one unit of 32-bit logits, two of 16-bit ones.
+template <typename T>
+__global__ __launch_bounds__(256) void logprobs_stats(lp_args a) {
+    constexpr int RUN = run_of<T>, RUNS = CHUNK / 256 / RUN;
+    __shared__ float s_sum[2][4], s_max[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int at = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
+    const lp_entry q = entry_of(a, a.first + at);
+    if (q.row < 0) return;
+    const T* row = (const T*)a.logits + (size_t)q.row * a.stride;
+    const bool aligned = ((unsigned long long)row & 15ull) == 0;
+    float v[RUNS][RUN], top = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < RUNS; r++) load_run<T>(row, chunk * CHUNK + ((r * 4 + wave) * 64 + lane) * RUN, a.vocab, aligned, v[r]);
+#pragma unroll
+    for (int r = 0; r < RUNS; r++) {
+        float m = v[r][0];
+#pragma unroll
+        for (int e = 1; e < RUN; e++) m = fmaxf(m, v[r][e]);
+        if (a.top > 0) {
+            m = wave_max_f32<RUN == 4 ? 64 : 32>(m);
+            const int unit = chunk * CHUNK_UNITS + (r * 4 + wave) * (RUN / 4) + (RUN == 4 ? 0 : lane >> 5);
+            if ((lane & (RUN == 4 ? 63 : 31)) == 0 && unit < a.units) a.most[(size_t)at * a.units + unit] = m;
+        }
+        top = fmaxf(top, m);
+    }
+    top = wave_max_f32(top);
+    if (lane == 0) s_max[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+    // (a chunk of nothing but -inf: every weight is 0, and no difference of infinities is taken)
+    const float m = top == -INFINITY ? 0.f : top;
+    float s = 0.f, e2 = 0.f;
+#pragma unroll
+    for (int r = 0; r < RUNS; r++)
+#pragma unroll
+        for (int e = 0; e < RUN; e++) {
+            const float d = (v[r][e] - m) * a.c, w = __builtin_amdgcn_exp2f(d);
+            s += w;
+            e2 += w > 0.f ? w * d : 0.f;      // (0 times an infinity; a NaN is in s)
+        }
+    s = wave_sum_f32(s);
+    e2 = wave_sum_f32(e2);
+    if (lane == 0) { s_sum[0][wave] = s; s_sum[1][wave] = e2; }
+    __syncthreads();
+    if (tid == 0)
+        a.stats[(size_t)at * a.chunks + chunk] = {top, (s_sum[0][0] + s_sum[0][1]) + (s_sum[0][2] + s_sum[0][3]),
+                                                  (s_sum[1][0] + s_sum[1][1]) + (s_sum[1][2] + s_sum[1][3]), 0.f};
+}
+
+// Keys in the order of what is looked for: larger values first, then lower numbers; no two are equal, and 0 is none.
+typedef unsigned long long u64;
+__device__ __forceinline__ u64 key_of(float v, int number) {
+    unsigned u = __float_as_uint(v + 0.f);      // (-0 is 0)
+    u = (u & 0x80000000u) ? ~u : u | 0x80000000u;
+    return ((u64)u << 32) | (0xFFFFFFFFu - (unsigned)number);
+}
+__device__ __forceinline__ float key_value(u64 k) {
+    const unsigned u = (unsigned)(k >> 32);
+    return __uint_as_float((u & 0x80000000u) ? u & 0x7FFFFFFFu : ~u);
+}
+__device__ __forceinline__ int key_number(u64 k) { return (int)(0xFFFFFFFFu - (unsigned)k); }
+template <int O>
+__device__ __forceinline__ void max_step(u64& k) {
+    const u64 other = ((u64)lane_xor<O>((unsigned)(k >> 32)) << 32) | lane_xor<O>((unsigned)k);
+    k = other > k ? other : k;
+}
+__device__ __forceinline__ u64 wave_max_key(u64 k) {
+    max_step<32>(k);
+    max_step<16>(k);
+    max_step<8>(k);
+    max_step<4>(k);
+    max_step<2>(k);
+    max_step<1>(k);
+    return k;
+}
+// The k largest keys of a workgroup's n per thread (get(i): thread's i-th; 0: none), into out[] in LDS, in order.  A thread holds its largest
+// one; the thread whose key was the largest of all looks for its next.
+template <typename Get>
+__device__ __forceinline__ void select_keys(int k, int n, Get get, u64* out, u64 (&red)[2][4]) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    u64 best = 0;
+    for (int i = 0; i < n; i++) {
+        const u64 x = get(i);
+        best = x > best ? x : best;
+    }
+    for (int j = 0; j < k; j++) {
+        const u64 w = wave_max_key(best);
+        if (lane == 0) red[j & 1][wave] = w;
+        __syncthreads();
+        u64 top = red[j & 1][0];
+#pragma unroll
+        for (int x = 1; x < 4; x++) top = red[j & 1][x] > top ? red[j & 1][x] : top;
+        if (tid == 0) out[j] = top;
+        if (best == top && top != 0) {
+            best = 0;
+            for (int i = 0; i < n; i++) {
+                const u64 x = get(i);
+                if (x < top && x > best) best = x;
+            }
+        }
+    }
+    __syncthreads();
+}
+
+// An entry: the chunks joined, and what is asked of it.
+template <typename T>
+__global__ __launch_bounds__(256) void logprobs_join(lp_args a) {
+    extern __shared__ __attribute__((aligned(16))) float cand[];      // [top][UNIT] logits of the units that are read again
+    __shared__ float s_most[UNITS_LDS];
+    __shared__ u64 red[2][4], unit_key[HS_LOGPROBS_TOP], tok_key[HS_LOGPROBS_TOP];
+    __shared__ double s_red[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const lp_entry q = entry_of(a, a.first + blockIdx.x);
+    if (q.row == -1) return;
+    const size_t i = (size_t)a.first + blockIdx.x;
+    const T* row = (const T*)a.logits + (size_t)max(q.row, 0) * a.stride;
+    const bool aligned = ((unsigned long long)row & 15ull) == 0;
+    const lp_stat* st = a.stats + (size_t)blockIdx.x * a.chunks;
+    // (every wavefront for itself: the same sums)
+    float m = -INFINITY;
+    double s = 0., e = 0.;
+    if (q.row >= 0) {
+        for (int c = lane; c < a.chunks; c += 64) m = fmaxf(m, st[c].m);
+        m = wave_max_f32(m);
+        for (int c = lane; c < a.chunks; c += 64) {
+            const lp_stat x = st[c];
+            const float d = x.m == -INFINITY ? 0.f : (x.m - m) * a.c, w = __builtin_amdgcn_exp2f(d);
+            s += (double)w * x.s;
+            e += (double)w * x.e + (w > 0.f ? (double)d * w * x.s : 0.);
+        }
+        s = wave_sum_f64(s);
+        e = wave_sum_f64(e);
+    }
+    const bool bad = q.row < 0 || !(s < INFINITY) || m == INFINITY, none = m == -INFINITY;
+    const double ln_s = bad || none ? 0. : log(s);
+    const float nan = __uint_as_float(0x7FC00000u);
+    auto logprob = [&](float l) { return bad ? nan : none || l == -INFINITY ? -INFINITY : (float)(((double)l - m) / a.t - ln_s); };
+    if (tid == 0) {
+        const bool inside = q.row >= 0 && (unsigned)q.token < (unsigned)a.vocab;
+        a.logprob[i] = logprob(inside ? wide(row[q.token]) : -INFINITY);
+        if (a.entropy) a.entropy[i] = bad ? nan : none ? 0.f : (float)(ln_s - e / s * 0.6931471805599453);
+    }
+    if (a.top == 0) return;
+    if (bad) {
+        if (tid < a.top) {
+            a.top_token[i * a.top + tid] = -1;
+            a.top_logprob[i * a.top + tid] = nan;
+        }
+        return;
+    }
+    const float* most = a.most + (size_t)blockIdx.x * a.units;
+    const int k_units = min(a.top, a.units), per = (a.units + 255) / 256;
+    if (a.units <= UNITS_LDS) {
+        for (int u = tid; u < a.units; u += 256) s_most[u] = most[u];
+        __syncthreads();
+        select_keys(k_units, per, [&](int j) { const int u = tid + 256 * j; return u < a.units ? key_of(s_most[u], u) : 0ull; }, unit_key, red);
+    } else {
+        select_keys(k_units, per, [&](int j) { const int u = tid + 256 * j; return u < a.units ? key_of(most[u], u) : 0ull; }, unit_key, red);
+    }
+    for (int u = wave; u < k_units; u += 4) {
+        const int base = key_number(unit_key[u]) * UNIT;
+#pragma unroll
+        for (int r = 0; r < UNIT / 64; r++) cand[u * UNIT + r * 64 + lane] = base + r * 64 + lane < a.vocab ? wide(row[base + r * 64 + lane]) : 0.f;
+    }
+    __syncthreads();
+    select_keys(a.top, k_units, [&](int u) {
+        const int t = key_number(unit_key[u]) * UNIT + tid;
+        return t < a.vocab ? key_of(cand[u * UNIT + tid], t) : 0ull;
+    }, tok_key, red);
+    if (tid < a.top) {
+        a.top_token[i * a.top + tid] = key_number(tok_key[tid]);
+        a.top_logprob[i * a.top + tid] = logprob(key_value(tok_key[tid]));
+    }
+}
+
+}  // namespace
+
+size_t hs_logprobs_scratch(int vocab) {
+    // what a call needs per entry; room for 16 MB of them, and for one at least
+    const size_t chunks = ((size_t)vocab + CHUNK - 1) / CHUNK, units = ((size_t)vocab + UNIT - 1) / UNIT;
+    return std::max<size_t>(16u << 20, chunks * sizeof(lp_stat) + units * 4);
+}
+
+void hs_launch_logprobs(const hs_ctx* ctx, const hs_logprobs_args* args, const hs_seq_state* seq, const hs_step* step, const void* logits,
+                        long long stride, int type, int rows, hipStream_t st) {
+    lp_args a = {};
+    a.logits = logits;
+    a.stride = (size_t)stride;
+    a.rows = rows;
+    a.vocab = ctx->desc.vocab;
+    a.top = args->top;
+    a.chunks = (a.vocab + CHUNK - 1) / CHUNK;
+    a.units = (a.vocab + UNIT - 1) / UNIT;
+    a.t = (double)args->temperature;
+    a.c = (float)(1.4426950408889634 / a.t);
+    a.row = args->row;
+    a.token = args->token;
+    a.live = args->live;
+    a.n = args->n;
+    if (args->emitted) {
+        a.row_off = step->row_off;
+        a.n_out = step->n_out;
+        a.out_tok = step->out_tok;
+        a.path_row = step->path_row;
+        a.k_stride = ctx->lim.k_max + 1;
+        a.batch = seq->batch;
+        a.n = a.batch * a.k_stride;
+    }
+    a.logprob = args->logprob;
+    a.entropy = args->entropy;
+    a.top_token = args->top_token;
+    a.top_logprob = args->top_logprob;
+    const size_t per = a.chunks * sizeof(lp_stat) + (a.top > 0 ? (size_t)a.units * 4 : 0);
+    const int most = (int)std::min<size_t>(hs_logprobs_scratch(a.vocab) / per, (1u << 23) / a.chunks);      // (a grid has fewer than 2^24 workgroups of 256)
+    char* scratch = ctx->ws + ctx->lay.logprobs;
+    const unsigned lds = (unsigned)std::min(a.top, a.units) * UNIT * 4;
+    for (a.first = 0; a.first < a.n; a.first += most) {
+        const int n = std::min(most, a.n - a.first);
+        a.stats = (lp_stat*)scratch;
+        a.most = (float*)(scratch + (size_t)n * a.chunks * sizeof(lp_stat));
+        if (type == HS_F32) {
+            hipLaunchKernelGGL((logprobs_stats<float>), dim3(n * a.chunks), dim3(256), 0, st, a);
+            hipLaunchKernelGGL((logprobs_join<float>), dim3(n), dim3(256), lds, st, a);
+        } else {
+            hipLaunchKernelGGL((logprobs_stats<bf16_t>), dim3(n * a.chunks), dim3(256), 0, st, a);
+            hipLaunchKernelGGL((logprobs_join<bf16_t>), dim3(n), dim3(256), lds, st, a);
+        }
+    }
+}

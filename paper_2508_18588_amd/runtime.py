@@ -14,7 +14,9 @@ from . import (HS_FLAG_WORKSPACE_LOGITS, hs_accept_commit, HS_FLAG_FP32_ACTIVATI
                hs_destroy, hs_draft, hs_draft_args, hs_draft_group, hs_group_draft_args, hs_get_profile, hs_kv_cache, hs_kv_commit, hs_limits,
                hs_model_desc, hs_policy, hs_poll_error, hs_prefill, hs_prefill_args, hs_seq_state, hs_set_flags, hs_set_profile, hs_step,
                hs_verify, hs_weights, hs_workspace_bytes, HS_BF16, HS_F32, hs_accept_probs, hs_accept_probs_args,
-               hs_attention_window, hs_probs, hs_probs_args, hs_set_window, hs_window_args)
+               hs_attention_window, hs_probs, hs_probs_args, hs_set_window, hs_window_args, hs_attention_shared, hs_logprobs,
+               hs_logprobs_args, hs_page_pool, hs_pages_compact, hs_pages_fork, hs_pages_free, hs_pages_reserve, hs_pages_scratch_bytes,
+               hs_set_shared_prefix, hs_shared_args, hs_shared_prefix)
 
 
 @dataclass
@@ -60,11 +62,12 @@ class Engine:
     def __init__(self, shape, weights: dict, rope, max_batch: int, k_max: int, c_max: int, max_len: int,
                  w_max: int = 32, seq_caps=None, shuffle_pages_seed: int | None = None, n_layers: int | None = None,
                  keep_logits: bool = True, g_max: int = 0, max_rows: int | None = None, precise: bool = False,
-                 workspace_logits: bool = False):
+                 workspace_logits: bool = False, pages: int | None = None):
         """keep_logits: give every step a [max_rows, vocab] fp32 logits tensor (hs_step.logits); without it (and
         without workspace_logits, which keeps them inside the library's workspace) no logits array exists and the
         argmax comes out of the LM head's epilogue.  precise: run in the library's fp32-activation mode (plain
-        kernels, float KV cache)."""
+        kernels, float KV cache).  pages: the cache is a pool of so many pages, none of which a sequence holds yet (reserve(), fork(),
+        free_pages(), compact()); without it every sequence has pages for its maximum length from the start."""
         self.shape = shape
         self.dev = torch.device("cuda:0")
         L = len(weights["wqkv"]) if n_layers is None else n_layers
@@ -81,16 +84,18 @@ class Engine:
         caps = [max_len] * max_batch if seq_caps is None else list(seq_caps)
         need = [(c + nodes + 15) // 16 for c in caps]
         self.max_blocks = max(need)
-        self.n_blocks = int(sum(need))
+        self.n_blocks = int(sum(need)) if pages is None else int(pages)
         ids = np.arange(self.n_blocks, dtype=np.int32)
         if shuffle_pages_seed is not None:
             np.random.default_rng(shuffle_pages_seed).shuffle(ids)
         bt = np.full((max_batch, self.max_blocks), -1, np.int32)
         o = 0
-        for b, n in enumerate(need):
+        for b, n in enumerate(need if pages is None else []):
             bt[b, :n] = ids[o:o + n]
             o += n
         self.block_table = _dev(bt)
+        self.page_refs = None if pages is None else torch.zeros(self.n_blocks, dtype=torch.int32, device=self.dev)
+        self.shared = None
         kv_elems = L * self.n_blocks * shape.n_kv_heads * 16 * shape.head_dim
         self.precise = precise
         kv_dtype = torch.float32 if precise else torch.int16
@@ -119,6 +124,10 @@ class Engine:
             hs_set_flags(self.ctx, self.flags)   # before the workspace is sized
         self.workspace = None
         self._bind_workspace()
+        if self.page_refs is not None:
+            self._page_scratch = torch.empty(max(1, hs_pages_scratch_bytes(self.ctx, self.n_blocks)), dtype=torch.uint8, device=self.dev)
+            self.c_pool = hs_page_pool(self.page_refs.data_ptr(), self.block_table.data_ptr(), self._page_scratch.data_ptr())
+            self.live_pages = torch.zeros(1, dtype=torch.int32, device=self.dev)
         # ---- sequence state and step arrays
         i32 = dict(dtype=torch.int32, device=self.dev)
         B, M = max_batch, self.max_rows
@@ -369,6 +378,125 @@ class Engine:
         args = hs_accept_probs_args(p.data_ptr(), None if q is None else q.data_ptr(), p.stride(0), 0 if q is None else q.stride(0),
                                     _type(p), u_accept.data_ptr(), u_sample.data_ptr())
         hs_accept_probs(self.ctx, args, self.c_seq, self.c_step, self.stream())
+
+    # ---------------------------------------------------------------- shared prefixes, pages, log probabilities
+
+    def set_shared_prefix(self, group_off, prefix_len=None):
+        """verify() and attention_shared() read the first prefix_len[g] positions of sequences group_off[g] .. group_off[g + 1] - 1, which hold the
+        same pages there, once for all of them; group_off = None: no sequences share."""
+        if group_off is None:
+            self.shared = None
+            hs_set_shared_prefix(self.ctx, None)
+            return
+        off, pre = np.asarray(group_off, np.int64), np.asarray(prefix_len, np.int64)
+        if off.ndim != 1 or off.size < 2 or pre.shape != (off.size - 1,):
+            raise ValueError(f"{off.size} group bounds, {pre.size} prefixes")
+        if (np.diff(off) < 0).any() or off[0] < 0 or off[-1] > self.max_batch or (pre < 0).any() or (pre >= 1 << 31).any():
+            raise ValueError("groups must be ascending ranges of sequences, prefixes lengths")
+        arrays = _dev(off.astype(np.int32)), _dev(pre.astype(np.int32))
+        shared = hs_shared_prefix(off.size - 1, max(1, int(np.diff(off).max())), int(pre.max()), arrays[0].data_ptr(), arrays[1].data_ptr())
+        hs_set_shared_prefix(self.ctx, shared)
+        self.shared, self._shared_arrays = shared, arrays
+
+    def attention_shared(self, layer: int, q, out):
+        """One layer's attention for the queries q [rows, n_q_heads * head_dim] of the rows laid out in the step arrays, with the prefixes of
+        set_shared_prefix() read once per group.  How many rows there are is known on the device: q and out have at least as many."""
+        if self.shared is None:
+            raise ValueError("no shared prefixes are set")
+        if q.shape != out.shape or q.dim() != 2 or q.shape[1] != self.shape.n_q_heads * self.shape.head_dim:
+            raise ValueError(f"queries {tuple(q.shape)}, output {tuple(out.shape)}")
+        if q.dtype != out.dtype or q.dtype != (torch.float32 if self.precise else torch.bfloat16):
+            raise ValueError(f"queries and output of {q.dtype}, {out.dtype}")
+        if not (q.is_contiguous() and out.is_contiguous()):
+            raise ValueError("queries and output must be contiguous")
+        self._on_device(q, out)
+        hs_attention_shared(self.ctx, self.c_cache, self.c_seq, self.c_step,
+                            hs_shared_args(layer, self.shared, q.data_ptr(), out.data_ptr()), self.stream())
+
+    def _pooled(self, *arrays):
+        if self.page_refs is None:
+            raise ValueError("this engine's sequences hold their pages from the start: create it with pages=")
+        for t in arrays:
+            if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.numel() < self.batch:
+                raise ValueError(f"one int32 per sequence expected, got {t.dtype} of shape {tuple(t.shape)}")
+        self._on_device(*arrays)
+
+    def reserve(self, extra: int, first=None):
+        """Pages for the next `extra` positions of every sequence with budget left (before a step: 1 + c_max * k_max), and for those from first[b] on
+        (int32 on the device; before a prefill: what is cached already)."""
+        self._pooled(*([] if first is None else [first]))
+        hs_pages_reserve(self.ctx, self.c_cache, self.c_seq, self.c_pool, extra, None if first is None else first.data_ptr(), self.stream())
+
+    def fork(self, parent):
+        """Sequence b takes the text of sequence parent[b] (int32 on the device; b itself or a negative number: it stays): full pages are shared, the
+        last one is copied."""
+        self._pooled(parent)
+        hs_pages_fork(self.ctx, self.c_cache, self.c_seq, self.c_pool, parent.data_ptr(), self.stream())
+
+    def free_pages(self, first, end):
+        """Releases the pages of every sequence b that lie wholly in positions first[b] .. end[b] - 1 (int32 on the device)."""
+        self._pooled(first, end)
+        hs_pages_free(self.ctx, self.c_cache, self.c_seq, self.c_pool, first.data_ptr(), end.data_ptr(), self.stream())
+
+    def compact(self, moved=None):
+        """Moves the held pages to the lowest numbers; returns their number (int32 [1], on the device).  moved: int32 [n_blocks] for every page's new
+        number."""
+        self._pooled()
+        if moved is not None:
+            if moved.dtype != torch.int32 or not moved.is_contiguous() or moved.numel() < self.n_blocks:
+                raise ValueError(f"int32 per page expected, got {moved.dtype} of shape {tuple(moved.shape)}")
+            self._on_device(moved)
+        hs_pages_compact(self.ctx, self.c_cache, self.c_pool, self.live_pages.data_ptr(), None if moved is None else moved.data_ptr(), self.stream())
+        return self.live_pages
+
+    def _logprob_outputs(self, out, n: int):
+        """(top, addresses) of out's tensors: logprob and optionally entropy [n], top_token and top_logprob [n, top]."""
+        known = {"logprob": torch.float32, "entropy": torch.float32, "top_token": torch.int32, "top_logprob": torch.float32}
+        if "logprob" not in out or set(out) - set(known) or ("top_token" in out) != ("top_logprob" in out):
+            raise ValueError(f"outputs {sorted(out)}")
+        top = out["top_token"].shape[-1] if "top_token" in out else 0
+        for name, t in out.items():
+            rows = (t.numel() // top if top else 0) if name.startswith("top") else t.numel()
+            if t.dtype != known[name] or not t.is_contiguous() or rows < n or (name.startswith("top") and (t.dim() != 2 or t.shape[-1] != top)):
+                raise ValueError(f"{name}: {t.dtype} of shape {tuple(t.shape)} for {n} entries")
+        self._on_device(*out.values())
+        return top, [out[name].data_ptr() if name in out and out[name].numel() else None for name in known]
+
+    def _entries(self, name, t, n=None):
+        if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
+            raise ValueError(f"{name}: contiguous int32 expected, got {t.dtype} of shape {tuple(t.shape)}")
+        self._on_device(t)
+
+    def logprobs(self, logits, tokens, out: dict, temperature: float = 1.0, rows=None, live=None):
+        """Log probabilities of `tokens` (int32 [n]) under softmax(logits / temperature), float32 or bfloat16 [.., vocab]; rows: the row of
+        logits that each belongs to (int32 [n]; None: its own number); live: how many of them there are (int32 on the device).  out: float32 `logprob` and
+        optionally `entropy` [n]; int32 `top_token` and float32 `top_logprob` [n, top] for the largest alternatives."""
+        kind, n = _type(logits), tokens.numel()
+        if logits.shape[1] < self.shape.vocab or (rows is None and logits.shape[0] < n):
+            raise ValueError(f"logits {tuple(logits.shape)} for {n} tokens of a vocabulary of {self.shape.vocab}")
+        self._entries("tokens", tokens)
+        if rows is not None:
+            self._entries("rows", rows, n)
+        if live is not None:
+            self._entries("live", live.view(-1), 1)
+        self._on_device(logits)
+        top, to = self._logprob_outputs(out, n)
+        args = hs_logprobs_args(logits.data_ptr(), logits.stride(0), kind, logits.shape[0], n, 0, temperature, top,
+                                None if rows is None else rows.data_ptr(), tokens.data_ptr(), None if live is None else live.data_ptr(), *to)
+        hs_logprobs(self.ctx, args, None, None, self.stream())
+
+    def emitted_logprobs(self, out: dict, temperature: float = 1.0, logits=None):
+        """The same for the tokens that the step has emitted, entry b * (k_max + 1) + i the i-th one of sequence b (others are left as they are):
+        between accept() or accept_commit() and the next draft, under the logits that verify() kept or given ones of the step's rows."""
+        top, to = self._logprob_outputs(out, self.batch * (self.k_max + 1))
+        kind, stride, rows = HS_F32, 0, 0
+        if logits is not None:
+            kind, stride, rows = _type(logits), logits.stride(0), logits.shape[0]
+            if logits.shape[1] < self.shape.vocab:
+                raise ValueError(f"logits {tuple(logits.shape)} for a vocabulary of {self.shape.vocab}")
+            self._on_device(logits)
+        args = hs_logprobs_args(None if logits is None else logits.data_ptr(), stride, kind, rows, 0, 1, temperature, top, None, None, None, *to)
+        hs_logprobs(self.ctx, args, self.c_seq, self.c_step, self.stream())
 
     def poll_error(self) -> int:
         return hs_poll_error(self.ctx, self.stream())
