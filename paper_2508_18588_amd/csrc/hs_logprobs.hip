@@ -4,8 +4,8 @@
 //
 // Bound by memory: the logits are read once.  The first launch takes a vocabulary in chunks of 8192 tokens, a workgroup each, and leaves each chunk's
 // maximum, sum of exp and sum of x exp, and the largest logit of every unit of 256 tokens; the second joins the chunks in their order, in 64 bits.
-// A row's k largest tokens lie in the k units with the largest maxima (the lower unit first among equal ones): k units are in front of any
-// other one, each with a token that is in front of all of its tokens.  So the second launch reads k units again and nothing else.
+// A row's k largest tokens lie in units whose maximum is not below the k-th largest one (k units have a token as large): the second launch reads little
+// more than k units again.
 // Chunks and units belong to the vocabulary alone: a row's results have the same bits whatever else is asked.
 #include <algorithm>
 #include <cmath>
@@ -133,15 +133,12 @@ __global__ __launch_bounds__(256) void logprobs_stats(lp_args a) {
 
 // Keys in the order of what is looked for: larger values first, then lower numbers; no two are equal, and 0 is none.
 typedef unsigned long long u64;
-__device__ __forceinline__ u64 key_of(float v, int number) {
-    unsigned u = __float_as_uint(v + 0.f);      // (-0 is 0)
-    u = (u & 0x80000000u) ? ~u : u | 0x80000000u;
-    return ((u64)u << 32) | (0xFFFFFFFFu - (unsigned)number);
+__device__ __forceinline__ unsigned ordered(float v) {
+    const unsigned u = __float_as_uint(v + 0.f);      // (-0 is 0)
+    return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ float key_value(u64 k) {
-    const unsigned u = (unsigned)(k >> 32);
-    return __uint_as_float((u & 0x80000000u) ? u & 0x7FFFFFFFu : ~u);
-}
+__device__ __forceinline__ u64 key_of(float v, int number) { return ((u64)ordered(v) << 32) | (0xFFFFFFFFu - (unsigned)number); }
+__device__ __forceinline__ float value_of(unsigned u) { return __uint_as_float((u & 0x80000000u) ? u & 0x7FFFFFFFu : ~u); }
 __device__ __forceinline__ int key_number(u64 k) { return (int)(0xFFFFFFFFu - (unsigned)k); }
 template <int O>
 __device__ __forceinline__ void max_step(u64& k) {
@@ -157,10 +154,46 @@ __device__ __forceinline__ u64 wave_max_key(u64 k) {
     max_step<1>(k);
     return k;
 }
-// The k largest keys of a workgroup's n per thread (get(i): thread's i-th; 0: none), into out[] in LDS, in order.  A thread holds its largest
-// one; the thread whose key was the largest of all looks for its next.
+
+// What of a row's tokens is in the running is narrowed in steps that cost the same whatever k is.  256 threads look at a share each; the k-th largest
+// of their maxima is a lower bound of the k-th largest of all, and little more than k values are above it.  So: the units whose maximum
+// is not below such a bound, of these units' tokens those that are not (or, if still too many, not below the bound of their own), and
+// for each of these the number that are in front of it.  Where more are left than there is room for, because hundreds of logits are equal, they are
+// taken one by one.  (One by one for all rows: 32 of 7 rows took 150 us; in these steps 9.)
+constexpr int LEFT = 256;      // units or tokens in the running
+struct pick_lds {
+    unsigned most[256];        // a thread's maximum, in its order, the last bits the thread's number
+    unsigned bound;
+    int n_units, n_tokens;
+    int unit[LEFT];
+    u64 token[LEFT], out[HS_LOGPROBS_TOP], red[2][4];
+};
+// A lower bound of the k-th largest of the threads' maxima (ordered, 0: fewer than k have one), which 8 of the 32 bits more would make exact.
+__device__ __forceinline__ unsigned lower_bound(float m, int k, pick_lds& l) {
+    const int tid = threadIdx.x;
+    const unsigned none = ordered(-INFINITY);
+    const unsigned mine = (ordered(m) & ~255u) | (unsigned)tid;
+    l.most[tid] = mine;
+    if (tid == 0) l.bound = 0;
+    __syncthreads();
+    int in_front = 0;
+    const uint4* all = reinterpret_cast<const uint4*>(l.most);
+#pragma unroll 16
+    for (int i = 0; i < 64; i++) {
+        const uint4 x = all[i];
+        in_front += (x.x > mine) + (x.y > mine) + (x.z > mine) + (x.w > mine);
+    }
+    if (in_front == k - 1 && ordered(m) > none) l.bound = max(ordered(m) & ~255u, none + 1);
+    __syncthreads();
+    return l.bound;
+}
+// (what a bound lets through; without one: whatever is not excluded)
+__device__ __forceinline__ bool in_running(float v, unsigned bound) { return ordered(v) >= (bound ? bound : ordered(-INFINITY) + 1); }
+
+// The k first keys of those that get(i), i < n, gives the workgroup's threads, one after the other: a thread holds its largest one, and the thread whose
+// key is the largest of all looks for its next.
 template <typename Get>
-__device__ __forceinline__ void select_keys(int k, int n, Get get, u64* out, u64 (&red)[2][4]) {
+__device__ void one_by_one(int k, int n, Get get, pick_lds& l) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     u64 best = 0;
     for (int i = 0; i < n; i++) {
@@ -169,12 +202,12 @@ __device__ __forceinline__ void select_keys(int k, int n, Get get, u64* out, u64
     }
     for (int j = 0; j < k; j++) {
         const u64 w = wave_max_key(best);
-        if (lane == 0) red[j & 1][wave] = w;
+        if (lane == 0) l.red[j & 1][wave] = w;
         __syncthreads();
-        u64 top = red[j & 1][0];
+        u64 top = l.red[j & 1][0];
 #pragma unroll
-        for (int x = 1; x < 4; x++) top = red[j & 1][x] > top ? red[j & 1][x] : top;
-        if (tid == 0) out[j] = top;
+        for (int x = 1; x < 4; x++) top = l.red[j & 1][x] > top ? l.red[j & 1][x] : top;
+        if (tid == 0) l.out[j] = top;
         if (best == top && top != 0) {
             best = 0;
             for (int i = 0; i < n; i++) {
@@ -186,19 +219,81 @@ __device__ __forceinline__ void select_keys(int k, int n, Get get, u64* out, u64
     __syncthreads();
 }
 
+// The k first tokens of a row into l.out, in order.  unit(u): the largest logit of unit u.
+template <typename T, typename Unit>
+__device__ __forceinline__ void pick_tokens(const T* __restrict__ row, int vocab, int units, int k, Unit unit, pick_lds& l) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    if (tid == 0) l.n_units = l.n_tokens = 0;
+    float m = -INFINITY;
+    for (int u = tid; u < units; u += 256) m = fmaxf(m, unit(u));
+    unsigned bound = lower_bound(m, k, l);
+    for (int u = tid; u < units; u += 256)
+        if (in_running(unit(u), bound)) {
+            const int at = atomicAdd(&l.n_units, 1);
+            if (at < LEFT) l.unit[at] = u;
+        }
+    __syncthreads();
+    const int n_units = l.n_units;
+    auto token = [&](int q) { return l.unit[q] * UNIT + tid; };
+    auto logit = [&](int q) { return token(q) < vocab ? wide(row[token(q)]) : -INFINITY; };
+    bool fits = n_units <= LEFT;
+    for (int turn = 0; fits; turn++) {
+        if (turn == 1) {      // too many: the bound of these tokens themselves
+            float most = -INFINITY;
+#pragma unroll 4
+            for (int q = 0; q < n_units; q++) most = fmaxf(most, logit(q));
+            if (tid == 0) l.n_tokens = 0;
+            bound = max(bound, lower_bound(most, k, l));
+        }
+        if (turn == 0 && bound == 0 && n_units > 1) continue;      // (no bound: that of the tokens at once)
+#pragma unroll 4
+        for (int q = 0; q < n_units; q++) {
+            const float v = logit(q);
+            if (in_running(v, bound)) {
+                const int at = atomicAdd(&l.n_tokens, 1);
+                if (at < LEFT) l.token[at] = key_of(v, token(q));
+            }
+        }
+        __syncthreads();
+        if (l.n_tokens <= LEFT) break;
+        __syncthreads();
+        fits = turn == 0;
+    }
+    if (fits) {
+        const int n = l.n_tokens;
+        if (tid < n) {
+            const u64 mine = l.token[tid];
+            int in_front = 0;
+#pragma unroll 4
+            for (int i = 0; i < n; i++) in_front += l.token[i] > mine;
+            if (in_front < k) l.out[in_front] = mine;
+        }
+        // fewer than k that are not excluded: the first excluded tokens follow, which are among the first n + k
+        if (n < k && tid < 64) {
+            const bool gone = lane < vocab && wide(row[lane]) == -INFINITY;
+            const int at = n + __popcll(__ballot(gone) & ((1ull << lane) - 1));
+            if (gone && at < k) l.out[at] = key_of(-INFINITY, lane);
+        }
+        __syncthreads();
+        return;
+    }
+    one_by_one(min(k, units), (units + 255) / 256, [&](int j) { const int u = tid + 256 * j; return u < units ? key_of(unit(u), u) : 0ull; }, l);
+    if (tid < min(k, units)) l.unit[tid] = key_number(l.out[tid]);
+    __syncthreads();
+    one_by_one(k, min(k, units), [&](int q) { return token(q) < vocab ? key_of(logit(q), token(q)) : 0ull; }, l);
+}
+static_assert(2 * HS_LOGPROBS_TOP <= 64, "the first excluded tokens, by a wavefront");
+
 // An entry: the chunks joined, and what is asked of it.
 template <typename T>
 __global__ __launch_bounds__(256) void logprobs_join(lp_args a) {
-    extern __shared__ __attribute__((aligned(16))) float cand[];      // [top][UNIT] logits of the units that are read again
     __shared__ float s_most[UNITS_LDS];
-    __shared__ u64 red[2][4], unit_key[HS_LOGPROBS_TOP], tok_key[HS_LOGPROBS_TOP];
-    __shared__ double s_red[4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ __attribute__((aligned(16))) pick_lds l;
+    const int tid = threadIdx.x, lane = tid & 63;
     const lp_entry q = entry_of(a, a.first + blockIdx.x);
     if (q.row == -1) return;
     const size_t i = (size_t)a.first + blockIdx.x;
     const T* row = (const T*)a.logits + (size_t)max(q.row, 0) * a.stride;
-    const bool aligned = ((unsigned long long)row & 15ull) == 0;
     const lp_stat* st = a.stats + (size_t)blockIdx.x * a.chunks;
     // (every wavefront for itself: the same sums)
     float m = -INFINITY;
@@ -233,27 +328,17 @@ __global__ __launch_bounds__(256) void logprobs_join(lp_args a) {
         return;
     }
     const float* most = a.most + (size_t)blockIdx.x * a.units;
-    const int k_units = min(a.top, a.units), per = (a.units + 255) / 256;
     if (a.units <= UNITS_LDS) {
         for (int u = tid; u < a.units; u += 256) s_most[u] = most[u];
         __syncthreads();
-        select_keys(k_units, per, [&](int j) { const int u = tid + 256 * j; return u < a.units ? key_of(s_most[u], u) : 0ull; }, unit_key, red);
+        pick_tokens(row, a.vocab, a.units, a.top, [&](int u) { return s_most[u]; }, l);
     } else {
-        select_keys(k_units, per, [&](int j) { const int u = tid + 256 * j; return u < a.units ? key_of(most[u], u) : 0ull; }, unit_key, red);
+        pick_tokens(row, a.vocab, a.units, a.top, [&](int u) { return most[u]; }, l);
     }
-    for (int u = wave; u < k_units; u += 4) {
-        const int base = key_number(unit_key[u]) * UNIT;
-#pragma unroll
-        for (int r = 0; r < UNIT / 64; r++) cand[u * UNIT + r * 64 + lane] = base + r * 64 + lane < a.vocab ? wide(row[base + r * 64 + lane]) : 0.f;
-    }
-    __syncthreads();
-    select_keys(a.top, k_units, [&](int u) {
-        const int t = key_number(unit_key[u]) * UNIT + tid;
-        return t < a.vocab ? key_of(cand[u * UNIT + tid], t) : 0ull;
-    }, tok_key, red);
     if (tid < a.top) {
-        a.top_token[i * a.top + tid] = key_number(tok_key[tid]);
-        a.top_logprob[i * a.top + tid] = logprob(key_value(tok_key[tid]));
+        const u64 key = l.out[tid];
+        a.top_token[i * a.top + tid] = key_number(key);
+        a.top_logprob[i * a.top + tid] = logprob(value_of((unsigned)(key >> 32)));
     }
 }
 
@@ -297,17 +382,16 @@ void hs_launch_logprobs(const hs_ctx* ctx, const hs_logprobs_args* args, const h
     const size_t per = a.chunks * sizeof(lp_stat) + (a.top > 0 ? (size_t)a.units * 4 : 0);
     const int most = (int)std::min<size_t>(hs_logprobs_scratch(a.vocab) / per, (1u << 23) / a.chunks);      // (a grid has fewer than 2^24 workgroups of 256)
     char* scratch = ctx->ws + ctx->lay.logprobs;
-    const unsigned lds = (unsigned)std::min(a.top, a.units) * UNIT * 4;
     for (a.first = 0; a.first < a.n; a.first += most) {
         const int n = std::min(most, a.n - a.first);
         a.stats = (lp_stat*)scratch;
         a.most = (float*)(scratch + (size_t)n * a.chunks * sizeof(lp_stat));
         if (type == HS_F32) {
             hipLaunchKernelGGL((logprobs_stats<float>), dim3(n * a.chunks), dim3(256), 0, st, a);
-            hipLaunchKernelGGL((logprobs_join<float>), dim3(n), dim3(256), lds, st, a);
+            hipLaunchKernelGGL((logprobs_join<float>), dim3(n), dim3(256), 0, st, a);
         } else {
             hipLaunchKernelGGL((logprobs_stats<bf16_t>), dim3(n * a.chunks), dim3(256), 0, st, a);
-            hipLaunchKernelGGL((logprobs_join<bf16_t>), dim3(n), dim3(256), lds, st, a);
+            hipLaunchKernelGGL((logprobs_join<bf16_t>), dim3(n), dim3(256), 0, st, a);
         }
     }
 }
