@@ -37,8 +37,9 @@ void layout_workspace(hs_ctx* ctx) {
     w.q = take(M * qh * ab);
     w.attn = take(M * qh * ab);
     w.act = take(M * (size_t)d.d_ffn * ab);
-    w.part_o = take(M * d.n_q_heads * (size_t)ctx->max_parts * d.head_dim * 2);   // fp16
-    w.part_ml = take(M * d.n_q_heads * (size_t)ctx->max_parts * 2 * 4);
+    const size_t parts = (size_t)(ctx->max_parts + hs_shared_runs(ctx));   // (a shared prefix's runs behind a sequence's own partitions)
+    w.part_o = take(M * d.n_q_heads * parts * d.head_dim * 2);   // fp16
+    w.part_ml = take(M * d.n_q_heads * parts * 2 * 4);
     w.logits_bytes = hs_logits_in_workspace(ctx) ? M * (size_t)d.vocab * 4 : 0;
     w.logits = take(w.logits_bytes);
     w.rowmax = take(M * (size_t)hs_gemm_rowmax_groups(d.vocab) * 8);

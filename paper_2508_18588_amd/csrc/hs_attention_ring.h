@@ -263,7 +263,7 @@ __device__ __forceinline__ void begin_tile(row_tile<HD>& t) {
 // tile: it says that the tile has landed (every wavefront has waited for its share) and that its predecessor has been read, whose place is
 // refilled then.  idle: the wavefront has no rows, only its share of the tiles.
 // LONG: there may be more than WIN_RUN tiles (and the rows are a chunk's, whose masks are not loaded but computed).  all_lo, all_hi: see
-// walk_keys, for this wavefront's rows.  Behind the last tile of every part_keys keys done(): the rows' state is complete, and starts again.
+// walk_keys, for this wavefront's rows.  LATE: the rows are waited for when the pages' numbers are there and not before these are asked for.  Behind the last tile of every part_keys keys done(): the rows' state is complete, and starts again.
 constexpr int WIN_RING = 4, WIN_RUN = 512;      // tiles in LDS; tiles whose pages are looked up at a time
 template <int HD>
 struct win_lds {
@@ -279,7 +279,7 @@ __device__ __forceinline__ __attribute__((always_inline)) void load_pair(const u
                  : "s"(lds_off), "v"(off0), "v"(off1), "s"(base), "i"(add), "i"(add + 1024)
                  : "memory", "m0");
 }
-template <int HD, bool LONG, typename A, typename S, typename Done>
+template <int HD, bool LONG, bool LATE = false, typename A, typename S, typename Done>
 __device__ __forceinline__ void ring_keys(const A& a, const S& s, const int32_t* __restrict__ bt, int j, int k0, int k_end,
                                           int part_keys, int all_lo, int all_hi, row_tile<HD>& t, bool idle, win_lds<HD>& lds, Done done) {
     using T = sub_tile<HD>;
@@ -318,9 +318,11 @@ __device__ __forceinline__ void ring_keys(const A& a, const S& s, const int32_t*
         return sc;
     };
     // (waited for here: inside the loop the wait would be for every load in flight)
+    if constexpr (!LATE) {
 #pragma unroll
-    for (int ks = 0; ks < NKS; ks++) asm volatile("" : "+v"(t.qf[ks]));
-    if (!LONG) asm volatile("" : "+v"(t.anc), "+v"(t.lo));
+        for (int ks = 0; ks < NKS; ks++) asm volatile("" : "+v"(t.qf[ks]));
+        if (!LONG) asm volatile("" : "+v"(t.anc), "+v"(t.lo));
+    }
 
     int k_next = (k0 / part_keys + 1) * part_keys, k_first = k0, odd = 0;
     for (int t0 = 0; t0 < n_tiles; t0 += WIN_RUN) {
@@ -333,6 +335,11 @@ __device__ __forceinline__ void ring_keys(const A& a, const S& s, const int32_t*
             lds.page[i] = page < a.n_blocks ? page : -1;
         }
         __syncthreads();
+        if constexpr (LATE) {
+#pragma unroll
+            for (int ks = 0; ks < NKS; ks++) asm volatile("" : "+v"(t.qf[ks]));
+            asm volatile("" : "+v"(t.anc));
+        }
         // (read long before they are used, which is when they go to a scalar register: a trip to the LDS takes longer than the rest of a fetch)
         auto pages_of = [&](int i) __attribute__((always_inline)) { return *reinterpret_cast<const int2*>(&lds.page[2 * (i - t0)]); };
         int ahead = 0, f = t0, f_slot = 0, f_page = lds.page[pg];      // ahead: tiles asked for and not yet waited for

@@ -244,7 +244,9 @@ void hs_launch_accept_probs(const hs_ctx* ctx, const hs_accept_probs_args* args,
 size_t hs_logprobs_scratch(int vocab);
 void hs_launch_logprobs(const hs_ctx* ctx, const hs_logprobs_args* args, const hs_seq_state* seq, const hs_step* step, const void* logits,
                         long long stride, int type, int rows, hipStream_t st);
-// Attention of sequences that share prefixes (hs_shared.hip): partial results, and the launch that joins them.
+// Attention of sequences that share prefixes (hs_shared.hip): partial results, and the launch that joins them.  hs_shared_runs: how many partial results
+// per row the workspace has for the runs of a prefix.
+int hs_shared_runs(const hs_ctx* ctx);
 void hs_launch_shared_attention(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step,
                                 const hs_shared_prefix* pre, const void* q, void* out, hipStream_t st);
 void hs_launch_shared_merge(const hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step, const hs_shared_prefix* pre,

@@ -155,35 +155,40 @@ __device__ __forceinline__ u64 wave_max_key(u64 k) {
     return k;
 }
 
-// What of a row's tokens is in the running is narrowed in steps that cost the same whatever k is.  256 threads look at a share each; the k-th largest
+// What of a row's tokens is in the running is narrowed in steps that cost the same whatever k is.  128 pairs of threads look at a share each; the k-th largest
 // of their maxima is a lower bound of the k-th largest of all, and little more than k values are above it.  So: the units whose maximum
 // is not below such a bound, of these units' tokens those that are not (or, if still too many, not below the bound of their own), and
 // for each of these the number that are in front of it.  Where more are left than there is room for, because hundreds of logits are equal, they are
 // taken one by one.  (One by one for all rows: 32 of 7 rows took 150 us; in these steps 9.)
 constexpr int LEFT = 256;      // units or tokens in the running
 struct pick_lds {
-    unsigned most[256];        // a thread's maximum, in its order, the last bits the thread's number
+    unsigned most[256], pair[128];      // a thread's maximum in its order; a pair's, the last bits the pair's number
     unsigned bound;
     int n_units, n_tokens;
     int unit[LEFT];
     u64 token[LEFT], out[HS_LOGPROBS_TOP], red[2][4];
 };
-// A lower bound of the k-th largest of the threads' maxima (ordered, 0: fewer than k have one), which 8 of the 32 bits more would make exact.
+// A lower bound of the k-th largest of the pairs' maxima (ordered, 0: fewer than k have one), which 7 of the 32 bits more would make exact.  (By pairs of
+// threads and two of the four wavefronts: the bound of 256 maxima is a little higher and takes four times as many instructions.)
 __device__ __forceinline__ unsigned lower_bound(float m, int k, pick_lds& l) {
     const int tid = threadIdx.x;
     const unsigned none = ordered(-INFINITY);
-    const unsigned mine = (ordered(m) & ~255u) | (unsigned)tid;
-    l.most[tid] = mine;
+    l.most[tid] = ordered(m);
     if (tid == 0) l.bound = 0;
     __syncthreads();
-    int in_front = 0;
-    const uint4* all = reinterpret_cast<const uint4*>(l.most);
+    const unsigned top = tid < 128 ? max(l.most[tid], l.most[tid + 128]) : 0u, mine = (top & ~127u) | (unsigned)tid;
+    if (tid < 128) l.pair[tid] = mine;
+    __syncthreads();
+    if (tid < 128) {
+        int in_front = 0;
+        const uint4* all = reinterpret_cast<const uint4*>(l.pair);
 #pragma unroll 16
-    for (int i = 0; i < 64; i++) {
-        const uint4 x = all[i];
-        in_front += (x.x > mine) + (x.y > mine) + (x.z > mine) + (x.w > mine);
+        for (int i = 0; i < 32; i++) {
+            const uint4 x = all[i];
+            in_front += (x.x > mine) + (x.y > mine) + (x.z > mine) + (x.w > mine);
+        }
+        if (in_front == k - 1 && top > none) l.bound = max(top & ~127u, none + 1);
     }
-    if (in_front == k - 1 && ordered(m) > none) l.bound = max(ordered(m) & ~255u, none + 1);
     __syncthreads();
     return l.bound;
 }
@@ -246,13 +251,17 @@ __device__ __forceinline__ void pick_tokens(const T* __restrict__ row, int vocab
             bound = max(bound, lower_bound(most, k, l));
         }
         if (turn == 0 && bound == 0 && n_units > 1) continue;      // (no bound: that of the tokens at once)
-#pragma unroll 4
-        for (int q = 0; q < n_units; q++) {
-            const float v = logit(q);
-            if (in_running(v, bound)) {
-                const int at = atomicAdd(&l.n_tokens, 1);
-                if (at < LEFT) l.token[at] = key_of(v, token(q));
-            }
+        // (sixteen on their way: the units are no longer in the caches, and a trip to memory takes longer than the rest)
+        for (int q0 = 0; q0 < n_units; q0 += 16) {
+            float v[16];
+#pragma unroll
+            for (int q = 0; q < 16; q++) v[q] = q0 + q < n_units ? logit(q0 + q) : -INFINITY;
+#pragma unroll
+            for (int q = 0; q < 16; q++)
+                if (in_running(v[q], bound)) {
+                    const int at = atomicAdd(&l.n_tokens, 1);
+                    if (at < LEFT) l.token[at] = key_of(v[q], token(q0 + q));
+                }
         }
         __syncthreads();
         if (l.n_tokens <= LEFT) break;
@@ -289,16 +298,31 @@ template <typename T>
 __global__ __launch_bounds__(256) void logprobs_join(lp_args a) {
     __shared__ float s_most[UNITS_LDS];
     __shared__ __attribute__((aligned(16))) pick_lds l;
+    __shared__ double row_ln_s;
+    __shared__ float row_m;
+    __shared__ int row_kind;      // 1: nothing but -inf; 2: a NaN or +inf
     const int tid = threadIdx.x, lane = tid & 63;
     const lp_entry q = entry_of(a, a.first + blockIdx.x);
     if (q.row == -1) return;
     const size_t i = (size_t)a.first + blockIdx.x;
     const T* row = (const T*)a.logits + (size_t)max(q.row, 0) * a.stride;
     const lp_stat* st = a.stats + (size_t)blockIdx.x * a.chunks;
-    // (every wavefront for itself: the same sums)
-    float m = -INFINITY;
-    double s = 0., e = 0.;
-    if (q.row >= 0) {
+    const float nan = __uint_as_float(0x7FC00000u);
+    if (q.row < 0) {
+        if (tid == 0) {
+            a.logprob[i] = nan;
+            if (a.entropy) a.entropy[i] = nan;
+        }
+        if (tid < a.top) {
+            a.top_token[i * a.top + tid] = -1;
+            a.top_logprob[i * a.top + tid] = nan;
+        }
+        return;
+    }
+    // The chunks, by the first wavefront.  (What is picked from a row with a NaN or +inf meanwhile is not used.)
+    if (tid < 64) {
+        float m = -INFINITY;
+        double s = 0., e = 0.;
         for (int c = lane; c < a.chunks; c += 64) m = fmaxf(m, st[c].m);
         m = wave_max_f32(m);
         for (int c = lane; c < a.chunks; c += 64) {
@@ -309,24 +333,18 @@ __global__ __launch_bounds__(256) void logprobs_join(lp_args a) {
         }
         s = wave_sum_f64(s);
         e = wave_sum_f64(e);
-    }
-    const bool bad = q.row < 0 || !(s < INFINITY) || m == INFINITY, none = m == -INFINITY;
-    const double ln_s = bad || none ? 0. : log(s);
-    const float nan = __uint_as_float(0x7FC00000u);
-    auto logprob = [&](float l) { return bad ? nan : none || l == -INFINITY ? -INFINITY : (float)(((double)l - m) / a.t - ln_s); };
-    if (tid == 0) {
-        const bool inside = q.row >= 0 && (unsigned)q.token < (unsigned)a.vocab;
-        a.logprob[i] = logprob(inside ? wide(row[q.token]) : -INFINITY);
-        if (a.entropy) a.entropy[i] = bad ? nan : none ? 0.f : (float)(ln_s - e / s * 0.6931471805599453);
+        const bool bad = !(s < INFINITY) || m == INFINITY, none = m == -INFINITY;
+        const double ln_s = bad || none ? 0. : log(s);
+        if (tid == 0) {
+            row_m = m;
+            row_ln_s = ln_s;
+            row_kind = bad ? 2 : none ? 1 : 0;
+            const float l = (unsigned)q.token < (unsigned)a.vocab ? wide(row[q.token]) : -INFINITY;
+            a.logprob[i] = bad ? nan : l == -INFINITY ? -INFINITY : (float)(((double)l - m) / a.t - ln_s);
+            if (a.entropy) a.entropy[i] = bad ? nan : none ? 0.f : (float)(ln_s - e / s * 0.6931471805599453);
+        }
     }
     if (a.top == 0) return;
-    if (bad) {
-        if (tid < a.top) {
-            a.top_token[i * a.top + tid] = -1;
-            a.top_logprob[i * a.top + tid] = nan;
-        }
-        return;
-    }
     const float* most = a.most + (size_t)blockIdx.x * a.units;
     if (a.units <= UNITS_LDS) {
         for (int u = tid; u < a.units; u += 256) s_most[u] = most[u];
@@ -335,10 +353,12 @@ __global__ __launch_bounds__(256) void logprobs_join(lp_args a) {
     } else {
         pick_tokens(row, a.vocab, a.units, a.top, [&](int u) { return most[u]; }, l);
     }
-    if (tid < a.top) {
+    if (tid < a.top) {      // (behind a barrier of pick_tokens)
         const u64 key = l.out[tid];
-        a.top_token[i * a.top + tid] = key_number(key);
-        a.top_logprob[i * a.top + tid] = logprob(value_of((unsigned)(key >> 32)));
+        const float v = value_of((unsigned)(key >> 32));
+        const bool bad = row_kind == 2;
+        a.top_token[i * a.top + tid] = bad ? -1 : key_number(key);
+        a.top_logprob[i * a.top + tid] = bad ? nan : v == -INFINITY ? -INFINITY : (float)(((double)v - row_m) / a.t - row_ln_s);
     }
 }
 

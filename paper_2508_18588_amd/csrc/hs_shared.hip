@@ -18,6 +18,7 @@
 
 #include "hs_attention_ring.h"
 #include "hs_internal.h"
+#include "hs_lanes.h"
 
 using namespace hs_ring;
 
@@ -33,6 +34,7 @@ struct shr_args {
     int32_t* parts;                     // [batch] partial results of a sequence's rows; -1: they have their results
     int batch, n_groups, max_blocks, n_blocks, hq, hkv, sinks, part_keys, max_parts;
     int splits, prefix_tiles, prefix_units;      // runs of a prefix; groups of four row tiles per run in the grid; workgroups for prefixes
+    int own_units;                               // ... and in front of them those for own keys
     int runs, tiles;                             // workgroups per (sequence, KV head) that share its partitions, and groups of four row tiles
     bool whole;                                  // own keys are one partition
     size_t part_rows;
@@ -48,15 +50,19 @@ struct shr_span {
 // A group: its members, of which `leader` is the first that has rows, and its keys [0, P), in n_pre runs.
 struct group_info { int b0, b1, leader, P, n_pre; };
 __device__ __forceinline__ int wave_min(int v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o));
-    return v;
+    v = min(v, (int)lane_xor<32>((unsigned)v));
+    v = min(v, (int)lane_xor<16>((unsigned)v));
+    v = min(v, (int)lane_xor<8>((unsigned)v));
+    v = min(v, (int)lane_xor<4>((unsigned)v));
+    v = min(v, (int)lane_xor<2>((unsigned)v));
+    return min(v, (int)lane_xor<1>((unsigned)v));
 }
 __device__ __forceinline__ group_info load_group(const shr_args& a, int g, int lane) {
     group_info r;
     r.b0 = max(a.group_off[g], 0);
     r.b1 = min(a.group_off[g + 1], a.batch);
     int shortest = INT32_MAX, leader = INT32_MAX;
+    const int length = a.prefix_len[g];
     for (int b = r.b0 + lane; b < r.b1; b += 64) {
         const bool rows = a.row_off[b + 1] > a.row_off[b];
         if (rows) {
@@ -66,7 +72,7 @@ __device__ __forceinline__ group_info load_group(const shr_args& a, int g, int l
     }
     r.leader = wave_min(leader);
     shortest = wave_min(shortest);
-    const int most = min(min(a.prefix_len[g], shortest), a.max_blocks * 16);
+    const int most = min(min(length, shortest), a.max_blocks * 16);
     r.P = r.leader == INT32_MAX || a.splits == 0 ? 0 : max(most, 0) & ~31;
     r.P = hs_uniform(r.P);
     r.leader = hs_uniform(r.leader);
@@ -83,19 +89,122 @@ __device__ __forceinline__ group_info group_of(const shr_args& a, int b, int lan
     return load_group(a, n - 1, lane);
 }
 
-// A workgroup with up to four row tiles at a time: either a run of a group's prefix for rows of all members (the first prefix_units workgroups),
-// or partitions of a sequence's own keys for its rows.
+// As load_pair, but the caches may keep what is loaded: other workgroups read the same keys for other rows.
+__device__ __forceinline__ __attribute__((always_inline)) void load_pair_kept(const unsigned char* base, unsigned off0, unsigned off1, unsigned lds_off,
+                                                                              const int add) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3 offset:%4\n\tglobal_load_lds_dwordx4 %2, %3 offset:%5"
+                 :
+                 : "s"(lds_off), "v"(off0), "v"(off1), "s"(base), "i"(add), "i"(add + 1024)
+                 : "memory", "m0");
+}
+
+// Tiles first, ... of a prefix with a row tile per wavefront, all of whose rows see all keys.  Key tiles come two at a time through the halves of the
+// ring: one half is multiplied while the other one is filled.  There is a barrier for two tiles and not for each, between which wavefronts drift
+// apart, so that of the two of a SIMD one has products for the matrix unit while the other one computes weights.  idle: the wavefront has no rows,
+// only its share of the tiles.  page: room for the numbers of 2 STEP_RUN pages.
+constexpr int STEP_RUN = WIN_RUN;
+template <int HD>
+__device__ __forceinline__ void step_keys(const shr_args& a, const int32_t* __restrict__ bt, int j, int first, int n_tiles, row_tile<HD>& t, bool idle,
+                                          unsigned char* ring, int* page_of) {
+    using T = sub_tile<HD>;
+    constexpr int NKS = HD / 16, NDT = HD / 32, CPW = T::PAGE / 1024, STEP = WIN_RING / 2;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
+    // the wavefront's share of a step: both pages' K (is_v = 0) or V^T of a tile
+    const unsigned page_bytes = (unsigned)a.hkv * T::PAGE;
+    const int is_v = wave & 1, my_tile = wave >> 1;
+    const unsigned ring_off = (unsigned)(size_t)(hs_gemm_detail::lds_ptr_t)ring + my_tile * T::BYTES + is_v * T::V;
+    const unsigned char* base = reinterpret_cast<const unsigned char*>(is_v ? a.vc : a.kc) + (size_t)j * T::PAGE;
+    const unsigned from = is_v ? T::v_from(lane) : T::k_at(lane / (HD / 8), lane % (HD / 8));
+    const int key_row = (l32 & 16) | page_order(l32 & 15);
+    for (int u0 = 0; u0 < n_tiles; u0 += STEP_RUN) {
+        const int n = min(n_tiles - u0, STEP_RUN);
+        __syncthreads();      // (the ring and the pages have been read)
+        bool missing = false;
+        for (int i = tid; i < 2 * n; i += 256) {
+            const int page = bt[2 * (first + u0) + i];
+            page_of[i] = page < a.n_blocks ? page : -1;
+            missing |= page < 0 || page >= a.n_blocks;
+        }
+        const bool holes = __syncthreads_or(missing);
+#pragma unroll
+        for (int ks = 0; ks < NKS; ks++) asm volatile("" : "+v"(t.qf[ks]));      // (waited for here, see ring_keys)
+        auto fetch = [&](int at, int buf) __attribute__((always_inline)) {      // the step that begins with tile at
+            if (at + my_tile >= n) return;
+#pragma unroll
+            for (int pg = 0; pg < 2; pg++) {
+                const int page = max(__builtin_amdgcn_readfirstlane(page_of[2 * (at + my_tile) + pg]), 0);
+                const unsigned char* src = base + (size_t)page * page_bytes;
+                const unsigned dst = ring_off + buf * STEP * T::BYTES + pg * T::PAGE;
+#pragma unroll
+                for (int i = 0; i < CPW; i += 2) load_pair_kept(src, is_v ? from : from ^ T::k_step(i), is_v ? from : from ^ T::k_step(i + 1), dst, i * 1024);
+            }
+        };
+        fetch(0, 0);
+        for (int at = 0, buf = 0; at < n; at += STEP, buf ^= 1) {
+            // this step has landed (every wavefront has waited for its share), and the one before has been read
+            HS_WAIT_VMCNT(0);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            fetch(at + STEP, buf ^ 1);
+            if (idle) continue;
+            const unsigned char* step = ring + buf * STEP * T::BYTES;
+            auto scores = [&](int x) __attribute__((always_inline)) {
+                key_tile<HD> k;
+                int k_at = T::k_at(key_row, half);
+                asm volatile("" : "+v"(k_at));
+#pragma unroll
+                for (int ks = 0; ks < NKS; ks++) k.k[ks] = *reinterpret_cast<const bf16x8*>(step + x * T::BYTES + (k_at ^ (ks << 5)));
+                f32x16 sc;
+#pragma unroll
+                for (int e = 0; e < 16; e++) sc[e] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < NKS; ks++) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.k[ks], t.qf[ks], sc, 0, 0, 0);
+                return sc;
+            };
+            // (the next tile's first product needs nothing of this one's weights)
+            auto tile = [&](int x, f32x16& sc, f32x16& next) __attribute__((always_inline)) {
+                value_tile<HD> v;
+#pragma unroll
+                for (int pp = 0; pp < 2; pp++)
+#pragma unroll
+                    for (int dt = 0; dt < NDT; dt++)
+                        v.v[pp][dt] = *reinterpret_cast<const bf16x8*>(step + x * T::BYTES + T::V + pp * T::PAGE + dt * 1024 + T::v_at(l32, half));
+                if (holes) {      // pages that there are none of: their keys are not seen
+                    const int p0 = __builtin_amdgcn_readfirstlane(page_of[2 * (at + x)]), p1 = __builtin_amdgcn_readfirstlane(page_of[2 * (at + x) + 1]);
+#pragma unroll
+                    for (int e = 0; e < 16; e++)
+                        if ((e < 8 ? p0 : p1) < 0) sc[e] = -INFINITY;
+#pragma unroll
+                    for (int pp = 0; pp < 2; pp++)
+#pragma unroll
+                        for (int dt = 0; dt < NDT; dt++)
+                            if ((pp ? p1 : p0) < 0) v.v[pp][dt] = {};
+                }
+                const float alpha = take_scores<HD>(a, shr_span{}, t, sc, places{}, false, 0, half);
+                if (x + 1 < STEP) next = scores(x + 1);      // (beyond the run: of whatever lies there, not used)
+                bf16x8 pb[2];
+                take_probabilities<HD>(a, t, sc, alpha, pb);
+                take_values<HD>(t, v, pb);
+            };
+            f32x16 even = scores(0), odd;
+            tile(0, even, odd);
+            if (at + 1 < n) tile(1, odd, odd);
+        }
+    }
+}
+
+// A workgroup with up to four row tiles at a time: either partitions of a sequence's own keys for its rows (the first own_units workgroups),
+// or a run of a group's prefix for rows of all members.
 template <int HD>
 __global__ __launch_bounds__(256, 2) void shared_rows(shr_args a) {
     __shared__ __attribute__((aligned(1024))) win_lds<HD> lds;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
     const int G = a.hq / a.hkv;
-    const bool prefix = (int)blockIdx.x < a.prefix_units;
+    const bool prefix = (int)blockIdx.x >= a.own_units;
     int j, r0, R, b_table, tile0, tile_step, turn, k0, k_end, part_keys, c;
     bool direct = false;
     shr_span s = {0, 0, 0, 0};
     if (prefix) {
-        const int per = a.n_groups * a.hkv * a.splits, unit = blockIdx.x % per;
+        const int per = a.n_groups * a.hkv * a.splits, at = blockIdx.x - a.own_units, unit = at % per;
         const int split = unit % a.splits, g = unit / a.splits / a.hkv;
         j = unit / a.splits % a.hkv;
         const group_info gr = load_group(a, g, lane);
@@ -103,7 +212,7 @@ __global__ __launch_bounds__(256, 2) void shared_rows(shr_args a) {
         r0 = a.row_off[gr.b0];
         R = (a.row_off[gr.b1] - r0) * G;
         b_table = gr.leader;
-        tile0 = 4 * (blockIdx.x / per);
+        tile0 = 4 * (at / per);
         tile_step = 4 * a.prefix_tiles;
         turn = 0;
         const int tiles = gr.P >> 5;
@@ -114,16 +223,16 @@ __global__ __launch_bounds__(256, 2) void shared_rows(shr_args a) {
         s.L = s.total = gr.P;
         a.lag = 8.f;
     } else {
-        const int per = a.batch * a.hkv * a.runs, unit = (blockIdx.x - a.prefix_units) % per, first = (blockIdx.x - a.prefix_units) / per;
-        const int run = unit % a.runs;
-        j = unit / a.runs % a.hkv;
-        const int b = unit / a.runs / a.hkv;
+        const int per = a.batch * a.hkv * a.runs, unit = blockIdx.x % per, first = blockIdx.x / per;
+        const int pair = unit / a.runs, run = (unit + (pair >> 3)) % a.runs;      // (ids are dealt to eight XCDs in turn: none gets the same run of all)
+        j = pair % a.hkv;
+        const int b = pair / a.hkv;
         r0 = a.row_off[b];
         const int nn = a.row_off[b + 1] - r0;
-        if (nn <= 0) return;
         R = nn * G;
-        const group_info gr = group_of(a, b, lane);
         s.L = min(a.seq_len[b] - 1, INT32_MAX - (1 << 25));      // (sums with L stay in 32 bits: there are at most 2^25 rows)
+        const group_info gr = group_of(a, b, lane);              // (asked for before it is known whether there are rows: one trip to memory)
+        if (nn <= 0) return;
         s.total = s.L < 0 ? 0 : min(s.L + nn, a.max_blocks * 16);
         s.total = min(s.total, max(s.L, 0) + HS_MAX_NODES);       // (no row sees a slot beyond those of 64 nodes)
         part_keys = a.whole ? INT32_MAX / 2 : a.part_keys;
@@ -151,9 +260,13 @@ __global__ __launch_bounds__(256, 2) void shared_rows(shr_args a) {
         t.lo = 0;
         t.hi = s.L;
         begin_tile<HD>(t);
-        asm volatile("" : "+v"(t.anc));      // (waited for here, not in the loop)
         c = c_first;
-        ring_keys<HD, true>(a, s, bt, j, k0, k_end, part_keys, 0, s.L, t, rt >= nrt, lds, [&]() __attribute__((always_inline)) {
+        if (prefix) {
+            step_keys<HD>(a, bt, j, k0 >> 5, (k_end - k0) >> 5, t, rt >= nrt, lds.ring, lds.page);
+            put_partial<HD>(a, t, r0, rt, R, G, j, c, lane);
+            continue;
+        }
+        ring_keys<HD, true, true>(a, s, bt, j, k0, k_end, part_keys, 0, s.L, t, rt >= nrt, lds, [&]() __attribute__((always_inline)) {
             if (!direct) {
                 put_partial<HD>(a, t, r0, rt, R, G, j, c, lane);
                 begin_tile<HD>(t);
@@ -164,21 +277,34 @@ __global__ __launch_bounds__(256, 2) void shared_rows(shr_args a) {
     }
 }
 
-// Joins the partial results of a row's query heads in their order: a wavefront takes 512 / HD heads of a row, a lane eight elements of one, eight partial
-// results at a time.
-template <int HD>
+// Joins the partial results of a row's query heads in their order: a wavefront takes 512 / HD heads of a row, a lane eight elements of one, four partial
+// results at a time (a prefix has three runs as a rule), all of which are asked for before the first is used.  EARLY: with few rows there may be many,
+// sixteen of which are asked for before it is known how many there are, and whether there is the row: what a launch of a few rows takes is its chain
+// of round trips to memory.
+template <int HD, bool EARLY>
 __global__ __launch_bounds__(256) void shared_merge(shr_args a) {
-    constexpr int LANES = HD / 8, HEADS = 64 / LANES, AHEAD = 8;
+    constexpr int LANES = HD / 8, HEADS = 64 / LANES, AHEAD = EARLY ? 16 : 4;
     typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
     const int lane = threadIdx.x & 63, head = (blockIdx.y * 4 + (threadIdx.x >> 6)) * HEADS + lane / LANES;
     if ((blockIdx.y * 4 + (threadIdx.x >> 6)) * HEADS >= a.hq) return;
     for (int row = blockIdx.x; (size_t)row * a.hq < a.part_rows; row += gridDim.x) {
-        if (row >= a.row_off[a.batch]) return;
-        const int n = a.parts[a.row2seq[row]];
-        if (n < 0) continue;
         const size_t prow = (size_t)row * a.hq + min(head, a.hq - 1);
         const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + prow;
         const _Float16* po = a.part_o + prow * HD + 8 * (lane % LANES);
+        float2 x0[AHEAD];
+        f16x8 v0[AHEAD];
+        if constexpr (EARLY) {
+            // (in bounds whether the row and its partial results exist or not)
+#pragma unroll
+            for (int p = 0; p < AHEAD; p++) {
+                x0[p] = ml[min(p, a.max_parts - 1) * a.part_rows];
+                v0[p] = *reinterpret_cast<const f16x8*>(po + min(p, a.max_parts - 1) * a.part_rows * HD);
+            }
+            hs_loads_issued();
+        }
+        if (row >= a.row_off[a.batch]) return;
+        const int n = a.parts[a.row2seq[row]];
+        if (n < 0) continue;
         float top = -INFINITY, den = 0.f, acc[8];
 #pragma unroll
         for (int i = 0; i < 8; i++) acc[i] = 0.f;
@@ -187,13 +313,18 @@ __global__ __launch_bounds__(256) void shared_merge(shr_args a) {
             f16x8 v[AHEAD];
 #pragma unroll
             for (int p = 0; p < AHEAD; p++) {
-                const int at = min(p0 + p, n - 1);
-                x[p] = ml[at * a.part_rows];
-                v[p] = *reinterpret_cast<const f16x8*>(po + at * a.part_rows * HD);
+                if (EARLY && p0 == 0) {
+                    x[p] = x0[p];
+                    v[p] = v0[p];
+                } else if (p0 + p < n) {
+                    x[p] = ml[(p0 + p) * a.part_rows];
+                    v[p] = *reinterpret_cast<const f16x8*>(po + (p0 + p) * a.part_rows * HD);
+                }
             }
             float m = top;
 #pragma unroll
-            for (int p = 0; p < AHEAD; p++) m = fmaxf(m, x[p].x);
+            for (int p = 0; p < AHEAD; p++)
+                if (p0 + p < n) m = fmaxf(m, x[p].x);
             const float safe = m == -INFINITY ? 0.f : m;
             if (p0 > 0) {
                 const float alpha = fast_exp2(top - safe);
@@ -203,13 +334,13 @@ __global__ __launch_bounds__(256) void shared_merge(shr_args a) {
             }
             top = m;
 #pragma unroll
-            for (int p = 0; p < AHEAD; p++) {
-                if (p0 + p >= n) break;
-                const float w = fast_exp2(x[p].x - safe) * x[p].y;      // (the partial result is stored normalised)
-                den += w;
+            for (int p = 0; p < AHEAD; p++)
+                if (p0 + p < n) {
+                    const float w = fast_exp2(x[p].x - safe) * x[p].y;      // (the partial result is stored normalised)
+                    den += w;
 #pragma unroll
-                for (int i = 0; i < 8; i++) acc[i] += w * (float)v[p][i];
-            }
+                    for (int i = 0; i < 8; i++) acc[i] += w * (float)v[p][i];
+                }
         }
         if (head < a.hq) {
             const float inv = den == 0.f ? 0.f : 1.f / den;
@@ -223,31 +354,32 @@ __global__ __launch_bounds__(256) void shared_merge(shr_args a) {
 
 // How keys are cut and shared out: a function of the limits and of the hints that come with the prefixes (not of a step's rows), since the order of
 // a row's sums follows from it; and, from what rows to expect, how many workgroups a launch has.
-constexpr int SHARED_WHOLE_KEYS = 16000, SHARED_SHORT_KEYS = 160;
+//
+// Own keys are one walk per (sequence, KV head) where there are as many of these as compute units and no more keys than SHARED_WHOLE_KEYS behind the
+// longest prefix, or so few keys that the walk is as short as a second partial result's way: 128 sequences of up to 4096 own tokens, 4 KV heads,
+// 124 us, in partitions of 512 to 2048 keys by one to four workgroups 121 to 160; 256 sequences with drafts, 2048 own tokens, 178, 182 to 229; 7
+// sequences of up to 1900 tokens, 2 KV heads, 51 and 19.  With fewer sequences a workgroup per partition, as many as four for every compute unit.
+//
+// A prefix is cut into as many runs as make two workgroups for every compute unit, three at least, so that the last ones to start are short: 64 trees
+// of 17 nodes behind 8000 tokens, 8 KV heads, with 1, 2, 3, 4 and 5 runs 251, 229, 219, 234 and 229 us, the drafts 231, 182, 178, 182 and 182, single tokens
+// 148, 124, 127, 129 and 132 (more runs keep the long walks of own keys waiting), 7 sequences behind 700 tokens 26, 21, 20, 19 and 19.
+constexpr int SHARED_WHOLE_KEYS = 16000, SHARED_SHORT_KEYS = 160, SHARED_RUNS = 3, SHARED_RUN_TILES = 4;
 struct shr_plan { int part_keys, max_parts, splits; bool whole; };
 shr_plan plan_keys(const hs_ctx* ctx, const hs_shared_prefix* pre) {
     const hs_limits& l = ctx->lim;
     const hs_model_desc& d = ctx->desc;
     const long long cap = (long long)l.max_blocks_per_seq * 16, longest = std::min<long long>(pre->max_prefix, cap);
-    const long long span = std::max<long long>(cap - longest, 32), G = d.n_q_heads / d.n_kv_heads;
-    const long long rows = G * pre->max_members * (1 + l.c_max * l.k_max);
+    const long long span = std::max<long long>(cap - longest, 32), pairs = (long long)l.max_batch * d.n_kv_heads;
     shr_plan p;
-    // runs of a prefix: two workgroups per compute unit with 128 rows each, of 256 keys at least
-    const long long units = (long long)pre->n_groups * d.n_kv_heads * ((rows + 127) / 128);
-    long long splits = std::max(1ll, std::min(longest / 256, (2 * ctx->n_cu + units - 1) / units));
-    splits = std::min(splits, 32ll);
-    if (longest < 32) splits = 0;
-    const long long pairs = (long long)l.max_batch * d.n_kv_heads;
     p.whole = span <= (pairs >= ctx->n_cu ? SHARED_WHOLE_KEYS : SHARED_SHORT_KEYS);
-    // (one partition more than keys are cut into: the one that a prefix ends in)
     long long part = 2048;
-    while (part > 128 && pairs * ((span + part - 1) / part) < 4ll * ctx->n_cu) part /= 2;
-    auto own = [&](long long n) { return p.whole ? 1ll : (cap + n - 1) / n; };
-    while (own(part) + 1 > ctx->max_parts && part < cap) part *= 2;
-    splits = std::min(splits, ctx->max_parts - own(part));
-    p.splits = (int)std::max(0ll, splits);
-    p.part_keys = (int)part;
-    p.max_parts = std::max(ctx->max_parts, 1);
+    while (part > ctx->att_part && pairs * ((span + part - 1) / part) < 4ll * ctx->n_cu) part /= 2;
+    p.part_keys = (int)std::max<long long>(part, ctx->att_part);      // (a table's keys in partitions of att_part: max_parts)
+    p.max_parts = ctx->max_parts + hs_shared_runs(ctx);
+    const long long rows = (long long)(d.n_q_heads / d.n_kv_heads) * pre->max_members * (1 + l.c_max * l.k_max), tiles = longest / 32;
+    const long long units = (long long)pre->n_groups * d.n_kv_heads * ((rows + 127) / 128);
+    const long long want = std::max<long long>(SHARED_RUNS, (2 * ctx->n_cu + units - 1) / units);
+    p.splits = tiles == 0 ? 0 : (int)std::max(1ll, std::min({want, (long long)hs_shared_runs(ctx), tiles / SHARED_RUN_TILES}));
     return p;
 }
 
@@ -296,16 +428,23 @@ shr_args make_args(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const
         const long long cap = (long long)a.max_blocks * 16, own = (cap + a.part_keys - 1) / a.part_keys, pairs = (long long)a.batch * a.hkv;
         a.runs = (int)std::max(1ll, std::min(own, (8ll * ctx->n_cu + pairs - 1) / pairs));
     }
+    a.own_units = a.batch * a.hkv * a.runs * a.tiles;
     a.prefix_units = a.n_groups * a.hkv * a.splits * a.prefix_tiles;
     return a;
 }
 
 }  // namespace
 
+// (with few rows many runs; of 64 MB at most, and 32)
+int hs_shared_runs(const hs_ctx* ctx) {
+    const long long row = (long long)ctx->desc.n_q_heads * (ctx->desc.head_dim * 2 + 8) * ctx->lim.max_rows;
+    return (int)std::min(32ll, std::max(4ll, (64ll << 20) / row));
+}
+
 void hs_launch_shared_attention(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step,
                                 const hs_shared_prefix* pre, const void* q, void* out, hipStream_t st) {
     const shr_args a = make_args(ctx, layer, cache, seq, step, pre, q, out);
-    const dim3 grid((unsigned)(a.prefix_units + a.batch * a.hkv * a.runs * a.tiles));
+    const dim3 grid((unsigned)(a.own_units + a.prefix_units));
     if (ctx->desc.head_dim == 128) hipLaunchKernelGGL((shared_rows<128>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((shared_rows<64>), grid, dim3(256), 0, st, a);
 }
@@ -315,6 +454,12 @@ void hs_launch_shared_merge(const hs_ctx* ctx, const hs_kv_cache* cache, const h
     const shr_args a = make_args(ctx, 0, cache, seq, step, pre, nullptr, out);
     const int per = 4 * 512 / ctx->desc.head_dim, sets = (a.hq + per - 1) / per;      // heads of a workgroup, workgroups of a row
     const dim3 grid(hs_row_grid(ctx, 256, sets), sets);
-    if (ctx->desc.head_dim == 128) hipLaunchKernelGGL((shared_merge<128>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((shared_merge<64>), grid, dim3(256), 0, st, a);
+    const bool early = ctx->lim.max_rows <= HS_EARLY_ROWS;
+    if (ctx->desc.head_dim == 128) {
+        if (early) hipLaunchKernelGGL((shared_merge<128, true>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((shared_merge<128, false>), grid, dim3(256), 0, st, a);
+    } else {
+        if (early) hipLaunchKernelGGL((shared_merge<64, true>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((shared_merge<64, false>), grid, dim3(256), 0, st, a);
+    }
 }
