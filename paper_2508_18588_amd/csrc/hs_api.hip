@@ -132,7 +132,10 @@ bool prefix_ok(const hs_ctx* ctx, const hs_shared_prefix* p) {
 // What the calls on pages have in common.
 hs_status pages_ok(hs_ctx* ctx, const char* who, const hs_kv_cache* cache, const hs_page_pool* pool) {
     auto bad = [&](hs_status code, const char* what) {
-        ctx->err = std::string(who) + ": " + what;
+        try {
+            ctx->err = std::string(who) + ": " + what;
+        } catch (const std::bad_alloc&) {      // (the code says it, too)
+        }
         return code;
     };
     if (!ctx->ws) return bad(HS_ERR_CAPACITY, "no workspace bound");
@@ -144,11 +147,12 @@ hs_status pages_ok(hs_ctx* ctx, const char* who, const hs_kv_cache* cache, const
 }
 hs_status pages_ok(hs_ctx* ctx, const char* who, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_page_pool* pool) {
     if (const hs_status s = pages_ok(ctx, who, cache, pool); s != HS_OK) return s;
-    if (!seq_ok(ctx, seq) || seq->block_table != pool->table) {
+    if (seq_ok(ctx, seq) && seq->block_table == pool->table) return HS_OK;
+    try {
         ctx->err = std::string(who) + ": sequence state, or a block table that is not the pool's";
-        return HS_ERR_INVALID_ARG;
+    } catch (const std::bad_alloc&) {
     }
-    return HS_OK;
+    return HS_ERR_INVALID_ARG;
 }
 
 }  // namespace

@@ -170,7 +170,9 @@ struct pick_lds {
 };
 // A lower bound of the k-th largest of the pairs' maxima (ordered, 0: fewer than k have one), which 7 of the 32 bits more would make exact.  (By pairs of
 // threads and two of the four wavefronts: the bound of 256 maxima is a little higher and takes four times as many instructions.)
-__device__ __forceinline__ unsigned lower_bound(float m, int k, pick_lds& l) {
+// meanwhile(): for the last wavefront, which has nothing else to do.
+template <typename Meanwhile>
+__device__ __forceinline__ unsigned lower_bound(float m, int k, pick_lds& l, Meanwhile meanwhile) {
     const int tid = threadIdx.x;
     const unsigned none = ordered(-INFINITY);
     l.most[tid] = ordered(m);
@@ -188,6 +190,8 @@ __device__ __forceinline__ unsigned lower_bound(float m, int k, pick_lds& l) {
             in_front += (x.x > mine) + (x.y > mine) + (x.z > mine) + (x.w > mine);
         }
         if (in_front == k - 1 && top > none) l.bound = max(top & ~127u, none + 1);
+    } else if (tid >= 192) {
+        meanwhile();
     }
     __syncthreads();
     return l.bound;
@@ -224,14 +228,14 @@ __device__ void one_by_one(int k, int n, Get get, pick_lds& l) {
     __syncthreads();
 }
 
-// The k first tokens of a row into l.out, in order.  unit(u): the largest logit of unit u.
-template <typename T, typename Unit>
-__device__ __forceinline__ void pick_tokens(const T* __restrict__ row, int vocab, int units, int k, Unit unit, pick_lds& l) {
+// The k first tokens of a row into l.out, in order.  unit(u): the largest logit of unit u; meanwhile(): see lower_bound.
+template <typename T, typename Unit, typename Meanwhile>
+__device__ __forceinline__ void pick_tokens(const T* __restrict__ row, int vocab, int units, int k, Unit unit, pick_lds& l, Meanwhile meanwhile) {
     const int tid = threadIdx.x, lane = tid & 63;
     if (tid == 0) l.n_units = l.n_tokens = 0;
     float m = -INFINITY;
     for (int u = tid; u < units; u += 256) m = fmaxf(m, unit(u));
-    unsigned bound = lower_bound(m, k, l);
+    unsigned bound = lower_bound(m, k, l, meanwhile);
     for (int u = tid; u < units; u += 256)
         if (in_running(unit(u), bound)) {
             const int at = atomicAdd(&l.n_units, 1);
@@ -248,7 +252,7 @@ __device__ __forceinline__ void pick_tokens(const T* __restrict__ row, int vocab
 #pragma unroll 4
             for (int q = 0; q < n_units; q++) most = fmaxf(most, logit(q));
             if (tid == 0) l.n_tokens = 0;
-            bound = max(bound, lower_bound(most, k, l));
+            bound = max(bound, lower_bound(most, k, l, [] {}));
         }
         if (turn == 0 && bound == 0 && n_units > 1) continue;      // (no bound: that of the tokens at once)
         // (sixteen on their way: the units are no longer in the caches, and a trip to memory takes longer than the rest)
@@ -300,7 +304,7 @@ __global__ __launch_bounds__(256) void logprobs_join(lp_args a) {
     __shared__ __attribute__((aligned(16))) pick_lds l;
     __shared__ double row_ln_s;
     __shared__ float row_m;
-    __shared__ int row_kind;      // 1: nothing but -inf; 2: a NaN or +inf
+    __shared__ bool row_bad;      // (a NaN or +inf)
     const int tid = threadIdx.x, lane = tid & 63;
     const lp_entry q = entry_of(a, a.first + blockIdx.x);
     if (q.row == -1) return;
@@ -319,44 +323,50 @@ __global__ __launch_bounds__(256) void logprobs_join(lp_args a) {
         }
         return;
     }
-    // The chunks, by the first wavefront.  (What is picked from a row with a NaN or +inf meanwhile is not used.)
-    if (tid < 64) {
-        float m = -INFINITY;
-        double s = 0., e = 0.;
-        for (int c = lane; c < a.chunks; c += 64) m = fmaxf(m, st[c].m);
+    // The chunks, by one wavefront, which has asked for the first ones (and for the token's logit) before it is its turn.  (What is picked from a row with
+    // a NaN or +inf is not used.)
+    const lp_stat x0 = lane < a.chunks ? st[lane] : lp_stat{-INFINITY, 0.f, 0.f, 0.f};
+    const float own = (unsigned)q.token < (unsigned)a.vocab ? wide(row[q.token]) : -INFINITY;
+    auto join_chunks = [&]() {
+        float m = x0.m;
+        for (int c = lane + 64; c < a.chunks; c += 64) m = fmaxf(m, st[c].m);
         m = wave_max_f32(m);
-        for (int c = lane; c < a.chunks; c += 64) {
-            const lp_stat x = st[c];
+        double s = 0., e = 0.;
+        auto add = [&](const lp_stat& x) {
             const float d = x.m == -INFINITY ? 0.f : (x.m - m) * a.c, w = __builtin_amdgcn_exp2f(d);
             s += (double)w * x.s;
             e += (double)w * x.e + (w > 0.f ? (double)d * w * x.s : 0.);
-        }
+        };
+        add(x0);
+        for (int c = lane + 64; c < a.chunks; c += 64) add(st[c]);
         s = wave_sum_f64(s);
         e = wave_sum_f64(e);
         const bool bad = !(s < INFINITY) || m == INFINITY, none = m == -INFINITY;
         const double ln_s = bad || none ? 0. : log(s);
-        if (tid == 0) {
+        if (lane == 0) {
             row_m = m;
             row_ln_s = ln_s;
-            row_kind = bad ? 2 : none ? 1 : 0;
-            const float l = (unsigned)q.token < (unsigned)a.vocab ? wide(row[q.token]) : -INFINITY;
-            a.logprob[i] = bad ? nan : l == -INFINITY ? -INFINITY : (float)(((double)l - m) / a.t - ln_s);
+            row_bad = bad;
+            a.logprob[i] = bad ? nan : own == -INFINITY ? -INFINITY : (float)(((double)own - m) / a.t - ln_s);
             if (a.entropy) a.entropy[i] = bad ? nan : none ? 0.f : (float)(ln_s - e / s * 0.6931471805599453);
         }
+    };
+    if (a.top == 0) {
+        if (tid < 64) join_chunks();
+        return;
     }
-    if (a.top == 0) return;
     const float* most = a.most + (size_t)blockIdx.x * a.units;
     if (a.units <= UNITS_LDS) {
         for (int u = tid; u < a.units; u += 256) s_most[u] = most[u];
         __syncthreads();
-        pick_tokens(row, a.vocab, a.units, a.top, [&](int u) { return s_most[u]; }, l);
+        pick_tokens(row, a.vocab, a.units, a.top, [&](int u) { return s_most[u]; }, l, join_chunks);
     } else {
-        pick_tokens(row, a.vocab, a.units, a.top, [&](int u) { return most[u]; }, l);
+        pick_tokens(row, a.vocab, a.units, a.top, [&](int u) { return most[u]; }, l, join_chunks);
     }
     if (tid < a.top) {      // (behind a barrier of pick_tokens)
         const u64 key = l.out[tid];
         const float v = value_of((unsigned)(key >> 32));
-        const bool bad = row_kind == 2;
+        const bool bad = row_bad;
         a.top_token[i * a.top + tid] = bad ? -1 : key_number(key);
         a.top_logprob[i * a.top + tid] = bad ? nan : v == -INFINITY ? -INFINITY : (float)(((double)v - row_m) / a.t - row_ln_s);
     }

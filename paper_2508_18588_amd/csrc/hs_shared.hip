@@ -435,10 +435,10 @@ shr_args make_args(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const
 
 }  // namespace
 
-// (with few rows many runs; of 64 MB at most, and 32)
+// (with few rows many runs; of 64 MB, and 32, at most, and as many as every prefix has)
 int hs_shared_runs(const hs_ctx* ctx) {
     const long long row = (long long)ctx->desc.n_q_heads * (ctx->desc.head_dim * 2 + 8) * ctx->lim.max_rows;
-    return (int)std::min(32ll, std::max(4ll, (64ll << 20) / row));
+    return (int)std::min(32ll, std::max<long long>(SHARED_RUNS, (64ll << 20) / row));
 }
 
 void hs_launch_shared_attention(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step,

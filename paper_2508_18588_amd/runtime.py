@@ -67,7 +67,8 @@ class Engine:
         without workspace_logits, which keeps them inside the library's workspace) no logits array exists and the
         argmax comes out of the LM head's epilogue.  precise: run in the library's fp32-activation mode (plain
         kernels, float KV cache).  pages: the cache is a pool of so many pages, none of which a sequence holds yet (reserve(), fork(),
-        free_pages(), compact()); without it every sequence has pages for its maximum length from the start."""
+        free_pages(), compact(); load_sequences() leaves them as they are); without it every sequence has pages for its maximum length from the
+        start."""
         self.shape = shape
         self.dev = torch.device("cuda:0")
         L = len(weights["wqkv"]) if n_layers is None else n_layers
@@ -95,7 +96,7 @@ class Engine:
             o += n
         self.block_table = _dev(bt)
         self.page_refs = None if pages is None else torch.zeros(self.n_blocks, dtype=torch.int32, device=self.dev)
-        self.shared = None
+        self.shared = self._shared_arrays = None
         kv_elems = L * self.n_blocks * shape.n_kv_heads * 16 * shape.head_dim
         self.precise = precise
         kv_dtype = torch.float32 if precise else torch.int16
@@ -389,14 +390,18 @@ class Engine:
             hs_set_shared_prefix(self.ctx, None)
             return
         off, pre = np.asarray(group_off, np.int64), np.asarray(prefix_len, np.int64)
-        if off.ndim != 1 or off.size < 2 or pre.shape != (off.size - 1,):
+        if off.ndim != 1 or not 2 <= off.size <= self.max_batch + 1 or pre.shape != (off.size - 1,):
             raise ValueError(f"{off.size} group bounds, {pre.size} prefixes")
         if (np.diff(off) < 0).any() or off[0] < 0 or off[-1] > self.max_batch or (pre < 0).any() or (pre >= 1 << 31).any():
             raise ValueError("groups must be ascending ranges of sequences, prefixes lengths")
-        arrays = _dev(off.astype(np.int32)), _dev(pre.astype(np.int32))
-        shared = hs_shared_prefix(off.size - 1, max(1, int(np.diff(off).max())), int(pre.max()), arrays[0].data_ptr(), arrays[1].data_ptr())
+        # (the arrays stay where they are: a graph that was recorded with other groups still reads them; groups that it has more are of none)
+        if self._shared_arrays is None:
+            self._shared_arrays = [torch.zeros(self.max_batch + 1, dtype=torch.int32, device=self.dev) for _ in range(2)]
+        for t, a, rest in zip(self._shared_arrays, (off, pre), (off[-1], 0)):
+            t.copy_(torch.from_numpy(np.concatenate([a, np.full(self.max_batch + 1 - a.size, rest)]).astype(np.int32)))
+        shared = hs_shared_prefix(off.size - 1, max(1, int(np.diff(off).max())), int(pre.max()), *(t.data_ptr() for t in self._shared_arrays))
         hs_set_shared_prefix(self.ctx, shared)
-        self.shared, self._shared_arrays = shared, arrays
+        self.shared = shared
 
     def attention_shared(self, layer: int, q, out):
         """One layer's attention for the queries q [rows, n_q_heads * head_dim] of the rows laid out in the step arrays, with the prefixes of

@@ -125,6 +125,24 @@ def test_equal_logits_take_the_lowest_token(dtype):
     eng.close()
 
 
+@pytest.mark.parametrize("crowd", [40, 300, 2000, 9000])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_crowded_units(crowd, dtype):
+    """The largest logits lie together in fewer units than are looked for, and more of them than there is room for at a time; and one of them in
+    every unit."""
+    vocab = 60000
+    eng = make(vocab)
+    x = logits_of(4, vocab, crowd, torch.float32, 1.0)
+    x[0, 1000:1000 + crowd] += 30
+    x[1, vocab - crowd:] += 30
+    x[2, ::max(1, vocab // crowd)] += 30
+    x[3, 5:5 + crowd] = 40 + torch.arange(crowd, device="cuda:0") % 3
+    x, tok = x.to(dtype), tokens_of(4, vocab)
+    for top in (1, 20, 32):
+        compare(ask(eng, x, tok, 1.0, top), expect(x, tok, 1.0, top))
+    eng.close()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_excluded_tokens(dtype):
     vocab = 9000

@@ -263,7 +263,7 @@ def test_captured_and_replayed():
         eng.attention_shared(0, q, out)
     pre_dev = eng._shared_arrays[1]
     for pre in ([200, 64], [96, 0], [0, 32], [200, 64]):
-        pre_dev.copy_(torch.tensor(pre, dtype=torch.int32))
+        pre_dev[:2].copy_(torch.tensor(pre, dtype=torch.int32))
         out.zero_()
         g.replay()
         torch.cuda.synchronize()
@@ -274,9 +274,52 @@ def test_captured_and_replayed():
     eng.close()
 
 
+def test_a_graph_of_other_groups():
+    """Prefixes set anew leave the arrays that a recorded graph reads where they are; its groups that there are no more are empty."""
+    eng, lens, pars, q = build((8, 2, 64), [0, 2, 4, 5], [200, 64, 96], [50, 60, 70, 80, 90], [1, 2, 3, 1, 2], seed=18)
+    out = torch.zeros_like(q)
+    eng.attention_shared(0, q, out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        eng.attention_shared(0, q, out)
+    for off, pre in (([0, 2], [160]), ([2, 4], [64]), ([0, 2, 4, 5], [200, 64, 96])):
+        eng.set_shared_prefix(off, pre)
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        check(out, eng, lens, pars, q, ALL, 0)
+    eng.close()
+
+
+def test_text_beyond_the_table():
+    """Of a sequence that has outgrown its table a row sees what the table holds, in a prefix and in its own keys."""
+    eng, lens, pars, q = build((8, 2, 64), [0, 3], [128], [30, 40, 50], [1, 1, 1], seed=19)
+    cap = 16 * eng.max_blocks
+    for ahead in (1, 17, 5000, 2 ** 31 - 2 - cap):
+        eng.seq_len[1] = min(cap + ahead, 2 ** 31 - 1)
+        got = attend(eng, q)
+        there = eng.block_table.cpu().numpy().repeat(16, 1) >= 0      # (of the table's keys all that it has pages for)
+        out, mag = reference(eng, [lens[0], cap, lens[2]], pars, q, ALL, 0, blocked=lambda b: ~there[b])
+        assert ((got.double() - out).abs() <= bound(out, mag)).all()
+    eng.close()
+
+
+def test_plain_kernels_on_a_16_bit_cache():
+    import paper_2508_18588_amd as hs
+    eng, lens, pars, q = build((8, 2, 64), [0, 3], [100], [5, 60, 7], [1, 2, -4], seed=20)
+    want = attend(eng, q)
+    eng.set_flags(hs.HS_FLAG_REFERENCE_KERNELS)
+    plain = attend(eng, q)
+    check(plain, eng, lens, pars, q, ALL, 0)
+    eng.set_flags(0)
+    assert torch.equal(attend(eng, q), want)
+    eng.close()
+
+
 def test_refusals_from_python():
     eng, lens, pars, q = build((4, 2, 64), [0, 3], [64], [5, 6, 7], [1, 2, 1], seed=17)
-    for off, pre in (([0], []), ([0, 3], [1, 2]), ([0, 2, 1], [1, 1]), ([0, 4], [1]), ([-1, 3], [1]), ([0, 3], [-1]), ([0, 3], [2 ** 31])):
+    for off, pre in (([0], []), ([0, 3], [1, 2]), ([0, 2, 1], [1, 1]), ([0, 4], [1]), ([-1, 3], [1]), ([0, 3], [-1]), ([0, 3], [2 ** 31]), ([0, 1, 1, 2, 3], [1, 1, 1, 1])):
         with pytest.raises(ValueError):
             eng.set_shared_prefix(off, pre)
     with pytest.raises(ValueError):
