@@ -351,7 +351,116 @@ __device__ __forceinline__ int free_page(const page_args& a, const int* sums, in
     return w * WORD + bit;
 }
 
+// Small pools: one workgroup has the index in LDS and needs no launch for it.  (16384 pages: 16 of a thread's counts are on their way at once.)
+constexpr int SMALL_PAGES = 16384, SMALL_WORDS = SMALL_PAGES / WORD, SMALL_CHUNKS = SMALL_PAGES / CHUNK;
+struct small_index {
+    u64 bits[SMALL_WORDS];
+    uint32_t before[SMALL_WORDS], chunk[SMALL_CHUNKS];
+    int sums[SMALL_CHUNKS + 1];
+};
+// By 1024 threads; a's index is this one then.  between(): what is done while the counts are on their way.
+template <typename Between>
+__device__ __forceinline__ void build_small(page_args& a, small_index& x, Between between) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int ref[16];
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+        const int page = (wave * 16 + i) * WORD + lane;
+        ref[i] = page < a.n_blocks ? a.refs[page] : 0;
+    }
+    hs_loads_issued();
+    between();
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+        const u64 held = __ballot(ref[i] != 0);
+        if (lane == 0) {
+            x.bits[wave * 16 + i] = held;
+            x.before[wave * 16 + i] = (uint32_t)__popcll(held);
+        }
+    }
+    __syncthreads();
+    if (wave < SMALL_CHUNKS) {
+        const int n = (int)x.before[wave * 64 + lane], upto = wave_prefix(n, lane);
+        x.before[wave * 64 + lane] = (uint32_t)(upto - n);
+        if (lane == 63) x.chunk[wave] = (uint32_t)upto;
+    }
+    __syncthreads();
+    if (tid <= SMALL_CHUNKS) {
+        int sum = 0;
+        for (int c = 0; c < tid; c++) sum += (int)x.chunk[c];
+        x.sums[tid] = sum;
+    }
+    __syncthreads();
+    a.bits = x.bits;
+    a.before = x.before;
+    a.chunk = x.chunk;
+}
+
+// A few pages per sequence: a thread per sequence counts what it lacks, and takes what is free from its place on.  (Turnovers of 117 sequences and 2343
+// pages with a launch for the index and one of a wavefront per sequence: 64 us, with this one 61; of 4 sequences 18 and 15.)
+constexpr int SMALL_BATCH = 1024, SMALL_EXTRA = 48, SMALL_ENTRIES = (15 + SMALL_EXTRA + 15) / 16;
+__global__ __launch_bounds__(1024) void pages_reserve_small(page_args a) {
+    __shared__ small_index x;
+    __shared__ int waves[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int lo = 0, hi = 0, n = 0, r = 0;
+    bool missing[SMALL_ENTRIES] = {};
+    int32_t* row = a.table + (size_t)min(tid, a.batch - 1) * a.max_blocks;
+    build_small(a, x, [&] {
+        if (tid < a.batch) {
+            wanted(a, tid, lo, hi);
+            int page[SMALL_ENTRIES];
+#pragma unroll
+            for (int i = 0; i < SMALL_ENTRIES; i++) page[i] = lo + i < hi ? row[lo + i] : 0;
+#pragma unroll
+            for (int i = 0; i < SMALL_ENTRIES; i++) {
+                missing[i] = lo + i < hi && !is_page(a, page[i]);
+                n += missing[i];
+            }
+        }
+        r = wave_prefix(n, lane);
+        if (lane == 63) waves[wave] = r;
+        r -= n;
+    });
+    for (int w = 0; w < wave; w++) r += waves[w];
+    const int free = a.n_blocks - x.sums[a.chunks];
+#pragma unroll
+    for (int i = 0; i < SMALL_ENTRIES; i++) {
+        if (!missing[i]) continue;
+        const int page = r < free ? free_page(a, x.sums, r) : -1;
+        r++;
+        row[lo + i] = page;
+        if (page >= 0) a.refs[page] = 1;
+        else report(a, HS_DEV_PAGES_EXHAUSTED);
+    }
+}
+
 // Every page's number after the move: the k-th free page below n_live is taken by the k-th held one from n_live on.
+__device__ __forceinline__ void map_page(const page_args& a, const int* sums, int page) {
+    const int live = sums[a.chunks], low = held_before(a, sums, live);
+    if (page == 0) {
+        *a.n_moves = live - low;
+        if (a.n_live) *a.n_live = live;
+    }
+    int to = -1;
+    if ((a.bits[page / WORD] >> (page % WORD)) & 1ull) {
+        to = page;
+        if (page >= live) {
+            const int k = held_before(a, sums, page) - low;
+            to = free_page(a, sums, k);
+            a.pairs[2 * k] = page;
+            a.pairs[2 * k + 1] = to;
+            a.refs[to] = a.refs[page];
+            a.refs[page] = 0;
+        }
+    }
+    a.moved[page] = to;
+}
+__global__ __launch_bounds__(1024) void pages_map_small(page_args a) {
+    __shared__ small_index x;
+    build_small(a, x, [] {});
+    for (int page = threadIdx.x; page < a.n_blocks; page += 1024) map_page(a, x.sums, page);
+}
 constexpr int CHUNKS_MAX = HS_PAGES_MAX / CHUNK;
 __global__ __launch_bounds__(256) void pages_map(page_args a) {
     __shared__ int sums[CHUNKS_MAX + 1];
@@ -366,26 +475,8 @@ __global__ __launch_bounds__(256) void pages_map(page_args a) {
         if (lane == 0) sums[a.chunks] = carry;
     }
     __syncthreads();
-    const int live = sums[a.chunks], low = held_before(a, sums, live);
-    if (blockIdx.x == 0 && tid == 0) {
-        *a.n_moves = live - low;
-        if (a.n_live) *a.n_live = live;
-    }
     const int page = blockIdx.x * 256 + tid;
-    if (page >= a.n_blocks) return;
-    int to = -1;
-    if ((a.bits[page / WORD] >> (page % WORD)) & 1ull) {
-        to = page;
-        if (page >= live) {
-            const int k = held_before(a, sums, page) - low;
-            to = free_page(a, sums, k);
-            a.pairs[2 * k] = page;
-            a.pairs[2 * k + 1] = to;
-            a.refs[to] = a.refs[page];
-            a.refs[page] = 0;
-        }
-    }
-    a.moved[page] = to;
+    if (page < a.n_blocks) map_page(a, sums, page);
 }
 // The tables' entries (the first max_batch workgroups) and the pages themselves, a run of (page, layer) each.
 __global__ __launch_bounds__(256) void pages_move(page_args a) {
@@ -474,6 +565,10 @@ void hs_launch_pages_reserve(const hs_ctx* ctx, const hs_kv_cache* cache, const 
     page_args a = make_args(ctx, cache, seq, pool);
     a.from = from;
     a.extra = extra;
+    if (!from && extra <= SMALL_EXTRA && a.batch <= SMALL_BATCH && a.n_blocks <= SMALL_PAGES) {
+        hipLaunchKernelGGL(pages_reserve_small, dim3(1), dim3(1024), 0, st, a);
+        return;
+    }
     hipLaunchKernelGGL((pages_index<INDEX_RESERVE>), dim3(a.chunks + (a.batch + 3) / 4), dim3(256), 0, st, a);
     hipLaunchKernelGGL(pages_reserve, dim3(a.batch), dim3(64), 0, st, a);
 }
@@ -482,8 +577,12 @@ void hs_launch_pages_compact(const hs_ctx* ctx, const hs_kv_cache* cache, const 
     page_args a = make_args(ctx, cache, nullptr, pool);
     a.n_live = n_live;
     if (moved) a.moved = moved;
-    hipLaunchKernelGGL((pages_index<INDEX_ONLY>), dim3(a.chunks), dim3(256), 0, st, a);
-    hipLaunchKernelGGL(pages_map, dim3((a.n_blocks + 255) / 256), dim3(256), 0, st, a);
+    if (a.n_blocks <= SMALL_PAGES) {
+        hipLaunchKernelGGL(pages_map_small, dim3(1), dim3(1024), 0, st, a);
+    } else {
+        hipLaunchKernelGGL((pages_index<INDEX_ONLY>), dim3(a.chunks), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(pages_map, dim3((a.n_blocks + 255) / 256), dim3(256), 0, st, a);
+    }
     const long long most = (long long)a.n_blocks / 2 * a.layers, wide = 8ll * ctx->n_cu;
     hipLaunchKernelGGL(pages_move, dim3((unsigned)(a.max_rows + std::max(1ll, std::min(most, wide)))), dim3(256), 0, st, a);
 }

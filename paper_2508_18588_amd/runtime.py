@@ -186,7 +186,8 @@ class Engine:
             self.ctx = None
 
     def stream(self):
-        return torch.cuda.current_stream().cuda_stream
+        # (of the engine's device; torch.cuda.current_stream() makes an object of it, 3 us a call)
+        return torch._C._cuda_getCurrentRawStream(self.dev.index)
 
     # ---------------------------------------------------------------- state loading (inputs only)
 
@@ -456,16 +457,17 @@ class Engine:
 
     def _logprob_outputs(self, out, n: int):
         """(top, addresses) of out's tensors: logprob and optionally entropy [n], top_token and top_logprob [n, top]."""
-        known = {"logprob": torch.float32, "entropy": torch.float32, "top_token": torch.int32, "top_logprob": torch.float32}
-        if "logprob" not in out or set(out) - set(known) or ("top_token" in out) != ("top_logprob" in out):
+        logprob, entropy, tokens, values = out.get("logprob"), out.get("entropy"), out.get("top_token"), out.get("top_logprob")
+        if logprob is None or (tokens is None) != (values is None) or len(out) != 4 - (entropy is None) - 2 * (tokens is None):
             raise ValueError(f"outputs {sorted(out)}")
-        top = out["top_token"].shape[-1] if "top_token" in out else 0
-        for name, t in out.items():
-            rows = (t.numel() // top if top else 0) if name.startswith("top") else t.numel()
-            if t.dtype != known[name] or not t.is_contiguous() or rows < n or (name.startswith("top") and (t.dim() != 2 or t.shape[-1] != top)):
-                raise ValueError(f"{name}: {t.dtype} of shape {tuple(t.shape)} for {n} entries")
-        self._on_device(*out.values())
-        return top, [out[name].data_ptr() if name in out and out[name].numel() else None for name in known]
+        top = 0 if tokens is None else tokens.shape[-1]
+        for t, kind, width in ((logprob, torch.float32, 0), (entropy, torch.float32, 0), (tokens, torch.int32, top), (values, torch.float32, top)):
+            if t is None:
+                continue
+            if t.dtype != kind or not t.is_contiguous() or (t.numel() < n if width == 0 else t.dim() != 2 or t.shape[1] != width or t.shape[0] < n):
+                raise ValueError(f"{t.dtype} of shape {tuple(t.shape)} for {n} entries")
+        self._on_device(logprob, entropy, tokens, values)
+        return top, [None if t is None else t.data_ptr() or None for t in (logprob, entropy, tokens, values)]
 
     def _entries(self, name, t, n=None):
         if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
