@@ -180,10 +180,12 @@ __device__ __forceinline__ void step_keys(const shr_args& a, const int32_t* __re
                             if ((pp ? p1 : p0) < 0) v.v[pp][dt] = {};
                 }
                 const float alpha = take_scores<HD>(a, shr_span{}, t, sc, places{}, false, 0, half);
+                __builtin_amdgcn_s_setprio(1);
                 if (x + 1 < STEP) next = scores(x + 1);      // (beyond the run: of whatever lies there, not used)
                 bf16x8 pb[2];
                 take_probabilities<HD>(a, t, sc, alpha, pb);
                 take_values<HD>(t, v, pb);
+                __builtin_amdgcn_s_setprio(0);
             };
             f32x16 even = scores(0), odd;
             tile(0, even, odd);
@@ -192,80 +194,60 @@ __device__ __forceinline__ void step_keys(const shr_args& a, const int32_t* __re
     }
 }
 
-// A workgroup with up to four row tiles at a time: either partitions of a sequence's own keys for its rows (the first own_units workgroups),
-// or a run of a group's prefix for rows of all members.
+// A run of a group's prefix for rows of all members, four row tiles at a time.
 template <int HD>
-__global__ __launch_bounds__(256, 2) void shared_rows(shr_args a) {
-    __shared__ __attribute__((aligned(1024))) win_lds<HD> lds;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
-    const int G = a.hq / a.hkv;
-    const bool prefix = (int)blockIdx.x >= a.own_units;
-    int j, r0, R, b_table, tile0, tile_step, turn, k0, k_end, part_keys, c;
-    bool direct = false;
-    shr_span s = {0, 0, 0, 0};
-    if (prefix) {
-        const int per = a.n_groups * a.hkv * a.splits, at = blockIdx.x - a.own_units, unit = at % per;
-        const int split = unit % a.splits, g = unit / a.splits / a.hkv;
-        j = unit / a.splits % a.hkv;
-        const group_info gr = load_group(a, g, lane);
-        if (split >= gr.n_pre) return;
-        r0 = a.row_off[gr.b0];
-        R = (a.row_off[gr.b1] - r0) * G;
-        b_table = gr.leader;
-        tile0 = 4 * (at / per);
-        tile_step = 4 * a.prefix_tiles;
-        turn = 0;
-        const int tiles = gr.P >> 5;
-        k0 = 32 * (int)((long long)tiles * split / gr.n_pre);
-        k_end = 32 * (int)((long long)tiles * (split + 1) / gr.n_pre);
-        part_keys = INT32_MAX / 2;
-        c = split;
-        s.L = s.total = gr.P;
-        a.lag = 8.f;
-    } else {
-        const int per = a.batch * a.hkv * a.runs, unit = blockIdx.x % per, first = blockIdx.x / per;
-        const int pair = unit / a.runs, run = (unit + (pair >> 3)) % a.runs;      // (ids are dealt to eight XCDs in turn: none gets the same run of all)
-        j = pair % a.hkv;
-        const int b = pair / a.hkv;
-        r0 = a.row_off[b];
-        const int nn = a.row_off[b + 1] - r0;
-        R = nn * G;
-        s.L = min(a.seq_len[b] - 1, INT32_MAX - (1 << 25));      // (sums with L stay in 32 bits: there are at most 2^25 rows)
-        const group_info gr = group_of(a, b, lane);              // (asked for before it is known whether there are rows: one trip to memory)
-        if (nn <= 0) return;
-        s.total = s.L < 0 ? 0 : min(s.L + nn, a.max_blocks * 16);
-        s.total = min(s.total, max(s.L, 0) + HS_MAX_NODES);       // (no row sees a slot beyond those of 64 nodes)
-        part_keys = a.whole ? INT32_MAX / 2 : a.part_keys;
-        const int f = gr.P / part_keys;
-        const int n = min(s.total > gr.P ? (s.total + part_keys - 1) / part_keys - f : 0, a.max_parts - gr.n_pre);
-        direct = a.whole && gr.n_pre == 0;
-        if (threadIdx.x == 0 && run == 0 && j == 0 && first == 0) a.parts[b] = direct ? -1 : gr.n_pre + n;
-        const int c0 = (int)((long long)n * run / a.runs), c1 = (int)((long long)n * (run + 1) / a.runs);
-        if (!direct && c0 >= c1) return;
-        b_table = b;
-        tile0 = 4 * first;
-        tile_step = 4 * a.tiles;
-        turn = run + j + b;
-        k0 = max(gr.P, (f + c0) * part_keys);
-        k_end = n == 0 ? k0 : (int)min((long long)s.total, (long long)(f + c1) * part_keys);
-        c = gr.n_pre + c0;
-    }
-    const int32_t* bt = a.block_table + (size_t)b_table * a.max_blocks;
-    const int nrt = (R + 31) >> 5;
-    const int c_first = c;
-    for (int tg = tile0; tg < nrt; tg += tile_step) {
-        const int rt = tg + ((wave - turn) & 3);      // (wavefronts with rows are not the same ones everywhere)
+__device__ __forceinline__ void prefix_rows(const shr_args& args, win_lds<HD>& lds) {
+    shr_args a = args;
+    a.lag = 8.f;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int G = a.hq / a.hkv, per = a.n_groups * a.hkv * a.splits, at = blockIdx.x - a.own_units, unit = at % per;
+    const int split = unit % a.splits, g = unit / a.splits / a.hkv, j = unit / a.splits % a.hkv;
+    const group_info gr = load_group(a, g, lane);
+    if (split >= gr.n_pre) return;
+    const int r0 = a.row_off[gr.b0], R = (a.row_off[gr.b1] - r0) * G, nrt = (R + 31) >> 5, tiles = gr.P >> 5;
+    const int first = (int)((long long)tiles * split / gr.n_pre), end = (int)((long long)tiles * (split + 1) / gr.n_pre);
+    const int32_t* bt = a.block_table + (size_t)gr.leader * a.max_blocks;
+    for (int tg = 4 * (at / per); tg < nrt; tg += 4 * a.prefix_tiles) {
+        const int rt = tg + wave;
         row_tile<HD> t;
-        load_query_tile<HD>(a.q, prefix ? nullptr : a.anc_mask, r0, rt, R, G, a.hq, j, half, l32, t.qf, t.anc);
+        load_query_tile<HD>(a.q, nullptr, r0, rt, R, G, a.hq, j, lane >> 5, lane & 31, t.qf, t.anc);
+        begin_tile<HD>(t);
+        step_keys<HD>(a, bt, j, first, end - first, t, rt >= nrt, lds.ring, lds.page);
+        put_partial<HD>(a, t, r0, rt, R, G, j, split, lane);
+    }
+}
+
+// Partitions of a sequence's own keys for its rows.
+template <int HD>
+__device__ __forceinline__ void own_rows(const shr_args& a, win_lds<HD>& lds) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int per = a.batch * a.hkv * a.runs, unit = blockIdx.x % per, first = blockIdx.x / per;
+    const int pair = unit / a.runs, run = (unit + (pair >> 3)) % a.runs;      // (ids are dealt to eight XCDs in turn: none gets the same run of all)
+    const int j = pair % a.hkv, b = pair / a.hkv, G = a.hq / a.hkv;
+    const int r0 = a.row_off[b], nn = a.row_off[b + 1] - r0, R = nn * G, nrt = (R + 31) >> 5;
+    shr_span s = {0, 0, 0, 0};
+    s.L = min(a.seq_len[b] - 1, INT32_MAX - (1 << 25));      // (sums with L stay in 32 bits: there are at most 2^25 rows)
+    const group_info gr = group_of(a, b, lane);              // (asked for before it is known whether there are rows: one trip to memory)
+    if (nn <= 0) return;
+    s.total = s.L < 0 ? 0 : min(s.L + nn, a.max_blocks * 16);
+    s.total = min(s.total, max(s.L, 0) + HS_MAX_NODES);       // (no row sees a slot beyond those of 64 nodes)
+    const int part_keys = a.whole ? INT32_MAX / 2 : a.part_keys, f = gr.P / part_keys;
+    const int n = min(s.total > gr.P ? (s.total + part_keys - 1) / part_keys - f : 0, a.max_parts - gr.n_pre);
+    const bool direct = a.whole && gr.n_pre == 0;
+    if (threadIdx.x == 0 && run == 0 && j == 0 && first == 0) a.parts[b] = direct ? -1 : gr.n_pre + n;
+    const int c0 = (int)((long long)n * run / a.runs), c1 = (int)((long long)n * (run + 1) / a.runs);
+    if (!direct && c0 >= c1) return;
+    const int k0 = max(gr.P, (f + c0) * part_keys);
+    const int k_end = n == 0 ? k0 : (int)min((long long)s.total, (long long)(f + c1) * part_keys);
+    const int32_t* bt = a.block_table + (size_t)b * a.max_blocks;
+    for (int tg = 4 * first; tg < nrt; tg += 4 * a.tiles) {
+        const int rt = tg + ((wave - (run + j + b)) & 3);      // (wavefronts with rows are not the same ones everywhere)
+        int c = gr.n_pre + c0;
+        row_tile<HD> t;
+        load_query_tile<HD>(a.q, a.anc_mask, r0, rt, R, G, a.hq, j, lane >> 5, lane & 31, t.qf, t.anc);
         t.lo = 0;
         t.hi = s.L;
         begin_tile<HD>(t);
-        c = c_first;
-        if (prefix) {
-            step_keys<HD>(a, bt, j, k0 >> 5, (k_end - k0) >> 5, t, rt >= nrt, lds.ring, lds.page);
-            put_partial<HD>(a, t, r0, rt, R, G, j, c, lane);
-            continue;
-        }
         ring_keys<HD, true, true>(a, s, bt, j, k0, k_end, part_keys, 0, s.L, t, rt >= nrt, lds, [&]() __attribute__((always_inline)) {
             if (!direct) {
                 put_partial<HD>(a, t, r0, rt, R, G, j, c, lane);
@@ -275,6 +257,15 @@ __global__ __launch_bounds__(256, 2) void shared_rows(shr_args a) {
         });
         if (direct) put_result<HD>(a, t, r0, rt, R, G, j, lane);
     }
+}
+
+// Workgroups for own keys, which memory bounds, and behind them those for prefixes, which the matrix unit bounds: the ones' loads and the others'
+// products overlap.
+template <int HD>
+__global__ __launch_bounds__(256, 2) void shared_rows(shr_args a) {
+    __shared__ __attribute__((aligned(1024))) win_lds<HD> lds;
+    if ((int)blockIdx.x >= a.own_units) prefix_rows<HD>(a, lds);
+    else own_rows<HD>(a, lds);
 }
 
 // Joins the partial results of a row's query heads in their order: a wavefront takes 512 / HD heads of a row, a lane eight elements of one, four partial
