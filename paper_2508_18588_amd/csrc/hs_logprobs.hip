@@ -412,7 +412,8 @@ void hs_launch_logprobs(const hs_ctx* ctx, const hs_logprobs_args* args, const h
     const size_t per = a.chunks * sizeof(lp_stat) + (a.top > 0 ? (size_t)a.units * 4 : 0);
     const int most = (int)std::min<size_t>(hs_logprobs_scratch(a.vocab) / per, (1u << 23) / a.chunks);      // (a grid has fewer than 2^24 workgroups of 256)
     char* scratch = ctx->ws + ctx->lay.logprobs;
-    for (a.first = 0; a.first < a.n; a.first += most) {
+    for (long long first = 0; first < a.n; first += most) {
+        a.first = (int)first;
         const int n = std::min(most, a.n - a.first);
         a.stats = (lp_stat*)scratch;
         a.most = (float*)(scratch + (size_t)n * a.chunks * sizeof(lp_stat));

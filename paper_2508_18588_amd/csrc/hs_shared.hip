@@ -232,7 +232,7 @@ __device__ __forceinline__ void own_rows(const shr_args& a, win_lds<HD>& lds) {
     s.total = s.L < 0 ? 0 : min(s.L + nn, a.max_blocks * 16);
     s.total = min(s.total, max(s.L, 0) + HS_MAX_NODES);       // (no row sees a slot beyond those of 64 nodes)
     const int part_keys = a.whole ? INT32_MAX / 2 : a.part_keys, f = gr.P / part_keys;
-    const int n = min(s.total > gr.P ? (s.total + part_keys - 1) / part_keys - f : 0, a.max_parts - gr.n_pre);
+    const int n = min(s.total > gr.P ? (s.total - 1) / part_keys + 1 - f : 0, a.max_parts - gr.n_pre);
     const bool direct = a.whole && gr.n_pre == 0;
     if (threadIdx.x == 0 && run == 0 && j == 0 && first == 0) a.parts[b] = direct ? -1 : gr.n_pre + n;
     const int c0 = (int)((long long)n * run / a.runs), c1 = (int)((long long)n * (run + 1) / a.runs);
