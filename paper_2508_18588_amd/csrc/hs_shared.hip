@@ -10,7 +10,10 @@
 // by each member through its own table.
 //
 // With 16 responses of one token, 28 query and 4 KV heads, a key is multiplied with 112 query rows per KV head: prefixes are bound by the matrix unit
-// and own keys by memory, and both kinds of workgroups are in one launch, so that the ones' products and the others' loads overlap.
+// and own keys by memory, and both kinds of workgroups are in one launch, so that the ones' products and the others' loads overlap.  Times here
+// are those of both launches.  16 prompts of 1500 to 4500 tokens, 16 sequences each with drafts and up to 2048 own tokens, 4 KV heads: prefixes alone
+// 108 us, own keys alone 115 (4.2 TB/s), together 163; 64 trees of 17 nodes behind 8000 tokens, 40 and 8 heads: 209 us, 200 of them the prefix
+// (880 TFLOP/s; the matrix unit is busy 47 % of the time, the vector unit 53 %, LDS 24 %, two wavefronts per SIMD to overlap them).
 //
 // The order of a row's sums is that of its keys: 32-key tiles; the runs of a prefix, which depend on its length, the limits and the hints given with
 // the prefixes; own keys in partitions at multiples of part_keys.  It does not depend on what other rows there are.
@@ -100,7 +103,8 @@ __device__ __forceinline__ __attribute__((always_inline)) void load_pair_kept(co
 
 // Tiles first, ... of a prefix with a row tile per wavefront, all of whose rows see all keys.  Key tiles come two at a time through the halves of the
 // ring: one half is multiplied while the other one is filled.  There is a barrier for two tiles and not for each, between which wavefronts drift
-// apart, so that of the two of a SIMD one has products for the matrix unit while the other one computes weights.  idle: the wavefront has no rows,
+// apart, so that of the two of a SIMD one has products for the matrix unit while the other one computes weights.  (With a barrier for each, as in
+// ring_keys, the trees took 249 us; so 216, and 208 since wavefronts with products go first and nothing of own_rows is live here.)  idle: the wavefront has no rows,
 // only its share of the tiles.  page: room for the numbers of 2 STEP_RUN pages.
 constexpr int STEP_RUN = WIN_RUN;
 template <int HD>
@@ -263,7 +267,7 @@ __device__ __forceinline__ void own_rows(const shr_args& a, win_lds<HD>& lds) {
 }
 
 // Workgroups for own keys, which memory bounds, and behind them those for prefixes, which the matrix unit bounds: the ones' loads and the others'
-// products overlap.
+// products overlap.  (Prefixes in front: the drafts 184 us instead of 163, the trees 213 instead of 209.)
 template <int HD>
 __global__ __launch_bounds__(256, 2) void shared_rows(shr_args a) {
     __shared__ __attribute__((aligned(1024))) win_lds<HD> lds;
@@ -351,12 +355,12 @@ __global__ __launch_bounds__(256) void shared_merge(shr_args a) {
 //
 // Own keys are one walk per (sequence, KV head) where there are as many of these as compute units and no more keys than SHARED_WHOLE_KEYS behind the
 // longest prefix, or so few keys that the walk is as short as a second partial result's way: 128 sequences of up to 4096 own tokens, 4 KV heads,
-// 124 us, in partitions of 512 to 2048 keys by one to four workgroups 121 to 160; 256 sequences with drafts, 2048 own tokens, 178, 182 to 229; 7
-// sequences of up to 1900 tokens, 2 KV heads, 51 and 19.  With fewer sequences a workgroup per partition, as many as four for every compute unit.
+// 125 us, in partitions of 512 to 2048 keys by one to four workgroups 117 to 161; 256 sequences with drafts, 2048 own tokens, 163, 168 to 200; 7
+// sequences of up to 1900 tokens, 2 KV heads, 52 and 16.  With fewer sequences a workgroup per partition, as many as four for every compute unit.
 //
 // A prefix is cut into as many runs as make two workgroups for every compute unit, three at least, so that the last ones to start are short: 64 trees
-// of 17 nodes behind 8000 tokens, 8 KV heads, with 1, 2, 3, 4 and 5 runs 251, 229, 219, 234 and 229 us, the drafts 231, 182, 178, 182 and 182, single tokens
-// 148, 124, 127, 129 and 132 (more runs keep the long walks of own keys waiting), 7 sequences behind 700 tokens 26, 21, 20, 19 and 19.
+// of 17 nodes behind 8000 tokens, 8 KV heads, with 1, 2, 3, 4 and 6 runs 232, 244, 209, 224 and 232 us, the drafts 232, 176, 163, 164 and 164, single tokens
+// 144, 121, 125, 127 and 129 (more runs keep the long walks of own keys waiting), 7 sequences behind 700 tokens 24, 19, 17, 16 and 16.
 constexpr int SHARED_WHOLE_KEYS = 16000, SHARED_SHORT_KEYS = 160, SHARED_RUNS = 3, SHARED_RUN_TILES = 4;
 struct shr_plan { int part_keys, max_parts, splits; bool whole; };
 shr_plan plan_keys(const hs_ctx* ctx, const hs_shared_prefix* pre) {
