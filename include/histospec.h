@@ -302,9 +302,10 @@ hs_status hs_attention_window(hs_ctx* ctx, const hs_kv_cache* cache, const hs_se
 
 /* Sequences that share a prefix: the responses to one prompt, whose block tables name the same pages for its tokens (hs_pages_fork makes such
  * tables).  Group g is the sequences group_off[g] .. group_off[g + 1] - 1, neighbours in the batch; the positions [0, prefix_len[g]) of all of its
- * members that have rows hold the same K and V in every layer, in pages that all of their tables name.  Groups are in ascending order and do not overlap; a group may be of one
- * sequence or of none, a sequence in no group; prefixes may have any length, and what of one a member has not cached yet (positions from seq_len - 1
- * on) is not shared by the group in that step.  The arrays are read by every call that follows them and stay the caller's. */
+ * members that have rows hold the same K and V in every layer, in pages that all of their tables name.  Groups are in ascending order and do not
+ * overlap; a group may be of one sequence or of none, a sequence in no group; prefixes may have any length, and what of one a member has not
+ * cached yet (positions from seq_len - 1 on) is not shared by the group in that step.  The arrays are read by every call that follows them and
+ * stay the caller's. */
 typedef struct hs_shared_prefix {
     int32_t n_groups;           /* HOST: 1..max_batch */
     int32_t max_members;        /* HOST: most sequences of a group, 1..max_batch: how launches are shaped, and with the next one how prefixes are */
@@ -314,19 +315,19 @@ typedef struct hs_shared_prefix {
 } hs_shared_prefix;
 
 /* hs_verify reads shared prefixes once per group instead of once per sequence from the next call on, in layers without a window (with the
- * plain-kernel flags and in layers with one every sequence reads its own table).  NULL: no sequences share.  The struct is copied; what a HIP graph has
- * recorded keeps it (the arrays' contents may change between replays).  Results are those without sharing but for the order of sums: a row's does not depend on what other rows
- * there are, but it does on prefix_len and the hints. */
+ * plain-kernel flags and in layers with one every sequence reads its own table).  NULL: no sequences share.  The struct is copied; what a HIP
+ * graph has recorded keeps it (the arrays' contents may change between replays).  Results are those without sharing but for the order of sums: a
+ * row's does not depend on what other rows there are, but it does on prefix_len and the hints. */
 hs_status hs_set_shared_prefix(hs_ctx* ctx, const hs_shared_prefix* prefix);
 
-/* Attention of one layer for queries that the caller has, with shared prefixes read once: what hs_verify runs when they are set.  row_off, row2seq,
- * pos and anc_mask of `step` are read, with the meaning that hs_draft gives them (at most 64 nodes per sequence).  A row sees the positions [0,
- * seq_len[b] - 1) and the nodes of its anc_mask:
- * out[row][h] = sum_t softmax_t(q[row][h] . k[t][h / G] / sqrt(head_dim)) v[t][h / G], G = n_q_heads / n_kv_heads; zeros for a row that sees nothing.
- * A position whose table entry is no page of the cache, or lies beyond the table, is not seen; what a row does not see has no influence on it,
- * infinities and NaNs included.  K and V of the rows themselves are read from the cache.  Rows from row_off[batch] on are left as they are.  With
- * HS_FLAG_FP32_ACTIVATIONS q and out are floats (and the cache is).  Partial results lie in the workspace: calls that share it are ordered by the
- * caller; the range of V that hs_verify states applies. */
+/* Attention of one layer for queries that the caller has, with shared prefixes read once: what hs_verify runs when they are set.  row_off,
+ * row2seq, pos and anc_mask of `step` are read, with the meaning that hs_draft gives them (at most 64 nodes per sequence).  A row sees the
+ * positions [0, seq_len[b] - 1) and the nodes of its anc_mask:
+ * out[row][h] = sum_t softmax_t(q[row][h] . k[t][h / G] / sqrt(head_dim)) v[t][h / G], G = n_q_heads / n_kv_heads; zeros for a row that sees
+ * nothing.  A position whose table entry is no page of the cache, or lies beyond the table, is not seen; what a row does not see has no influence
+ * on it, infinities and NaNs included.  K and V of the rows themselves are read from the cache.  Rows from row_off[batch] on are left as they
+ * are.  With HS_FLAG_FP32_ACTIVATIONS q and out are floats (and the cache is).  Partial results lie in the workspace: calls that share it are
+ * ordered by the caller; the range of V that hs_verify states applies. */
 typedef struct hs_shared_args {
     int32_t layer;
     hs_shared_prefix prefix;
@@ -336,10 +337,13 @@ typedef struct hs_shared_args {
 hs_status hs_attention_shared(hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step,
                               const hs_shared_args* args, hs_stream stream);
 
-/* The cache's pages as a pool.  refs[p] is the number of block-table entries that name page p, plus what the caller adds for holds of its own; a page with
- * 0 is free.  The caller zeroes refs and fills table with -1 before the first call (or sets both to what its tables hold).  Free pages are taken in
- * ascending order, for sequences in ascending order and for a sequence's positions in ascending order; pages that a call releases are free for the
- * next one.  Nothing is synchronised: what goes wrong on the device sets a bit of the error word.  All calls on one pool are ordered by the caller. */
+/* The cache's pages as a pool.  refs[p] is the number of block-table entries that name page p, plus what the caller adds for holds of its own; a
+ * page with 0 is free.  The caller zeroes refs and fills table with -1 before the first call (or sets both to what its tables hold).  Free pages
+ * are taken in ascending order, for sequences in ascending order and for a sequence's positions in ascending order; pages that a call releases are
+ * free for the next one.  Nothing is synchronised: what goes wrong on the device sets a bit of the error word.  All calls on one pool are ordered
+ * by the caller.  A page that several sequences name is one that all of them have filled: steps write behind it.  Before another text is put in a
+ * sequence's place (a new prompt, hs_prefill from positions in such pages) its pages are released, since what is written there would be the
+ * others' text, too. */
 enum { HS_PAGES_MAX = 1 << 22 };        /* pages of a pool */
 typedef struct hs_page_pool {
     int32_t* refs;      /* DEVICE [n_blocks] */
@@ -348,16 +352,17 @@ typedef struct hs_page_pool {
 } hs_page_pool;
 size_t hs_pages_scratch_bytes(const hs_ctx* ctx, int32_t n_blocks);     /* 0: n_blocks out of range */
 
-/* Releases the pages of sequence b that lie wholly in positions [from[b], to[b]) (from, to: DEVICE [batch]; to = INT32_MAX: to the end; from >= to:
- * none): their entries become -1 and they lose a reference.  An entry on a page without one sets HS_DEV_PAGE_REFUSED (and becomes -1). */
+/* Releases the pages of sequence b that lie wholly in positions [from[b], to[b]) (from, to: DEVICE [batch]; to = INT32_MAX: to the end; from >=
+ * to: none): their entries become -1 and they lose a reference.  An entry on a page without one sets HS_DEV_PAGE_REFUSED (and becomes -1). */
 hs_status hs_pages_free(hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_page_pool* pool, const int32_t* from,
                         const int32_t* to, hs_stream stream);
 
 /* Sequence b takes the text of sequence parent[b] (DEVICE [batch]; b itself or a negative number: it stays as it is): it shares the full pages of
- * what the parent has cached (positions [0, seq_len - 1)), gets a page of its own with a copy of the last, partly filled one (all layers), and holds nothing beyond;
- * what it held before is released.  seq_len, tail, tail_len, k_state, budget_left and the token log are copied, seq_id is not.  Entries of the parent
- * that are no pages are copied as -1.  Many sequences may have one parent.  Left as they are: sequences whose parent is not in the batch, takes another one's text in the
- * same call, has no tokens or has outgrown its table (HS_DEV_PAGE_REFUSED), and those for whose copy no page is left (HS_DEV_PAGES_EXHAUSTED). */
+ * what the parent has cached (positions [0, seq_len - 1)), gets a page of its own with a copy of the last, partly filled one (all layers), and
+ * holds nothing beyond; what it held before is released.  seq_len, tail, tail_len, k_state, budget_left and the token log are copied, seq_id is
+ * not.  Entries of the parent that are no pages are copied as -1.  Many sequences may have one parent.  Left as they are: sequences whose parent
+ * is not in the batch, takes another one's text in the same call, has no tokens or has outgrown its table (HS_DEV_PAGE_REFUSED), and those for
+ * whose copy no page is left (HS_DEV_PAGES_EXHAUSTED). */
 hs_status hs_pages_fork(hs_ctx* ctx, const hs_kv_cache* cache, hs_seq_state* seq, const hs_page_pool* pool, const int32_t* parent,
                         hs_stream stream);
 
@@ -368,9 +373,9 @@ hs_status hs_pages_reserve(hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_s
                            int32_t extra, hs_stream stream);
 
 /* Moves the held pages to the lowest numbers, so that the upper part of the cache can be given away: the k-th free page below n_live, the number
- * of held pages, takes what the k-th held page from n_live on has, in all layers; the entries of all max_batch rows of the table and the references follow.  n_live
- * (DEVICE, optional) receives that number, moved (DEVICE [n_blocks], optional) every page's new number, -1 for a free one: what the caller keeps of
- * its own is renamed by it. */
+ * of held pages, takes what the k-th held page from n_live on has, in all layers; the entries of all max_batch rows of the table and the
+ * references follow.  n_live (DEVICE, optional) receives that number, moved (DEVICE [n_blocks], optional) every page's new number, -1 for a free
+ * one: what the caller keeps of its own is renamed by it. */
 hs_status hs_pages_compact(hs_ctx* ctx, const hs_kv_cache* cache, const hs_page_pool* pool, int32_t* n_live, int32_t* moved, hs_stream stream);
 
 /* One target-model forward pass over all M rows (Sec. 2.2).  Writes every row's K/V into the cache at slot
@@ -430,12 +435,13 @@ typedef struct hs_probs_args {
 hs_status hs_probs(hs_ctx* ctx, const hs_probs_args* args, hs_stream stream);
 
 /* Log probabilities of tokens under softmax(logits / temperature), the entropies of these distributions in nats, and the `top` largest logits of a
- * row (the lowest token id first among equal ones) with theirs: what the trainer asks of a rollout's tokens.  Entry i of n asks about row
- * row[i] (NULL: i) and token[i]; rows may be asked in any order and more than once.  emitted != 0: entry b * (k_max + 1) + i is the i-th token that sequence b has
- * emitted in this step, i < n_out[b], out_tok[b][i] at the row of node path_row[b][i]: between acceptance and the next draft.  Entries that are not there
- * (i >= *live, i >= n_out[b]) are left as they are.  A token outside the vocabulary, or an excluded one (logit -inf), has -inf; a row of nothing else
- * -inf everywhere and entropy 0; a row with a NaN or +inf, or an index outside [0, rows), NaN and alternatives -1.  Sums of 8192 tokens are in 32 bits, all others
- * in 64; a row's results do not depend on what else is asked.  Scratch lies in the workspace: calls that share it are ordered by the caller. */
+ * row (the lowest token id first among equal ones) with theirs: what the trainer asks of a rollout's tokens.  Entry i of n asks about row row[i]
+ * (NULL: i) and token[i]; rows may be asked in any order and more than once.  emitted != 0: entry b * (k_max + 1) + i is the i-th token that
+ * sequence b has emitted in this step, i < n_out[b], out_tok[b][i] at the row of node path_row[b][i]: between acceptance and the next draft.
+ * Entries that are not there (i >= *live, i >= n_out[b]) are left as they are.  A token outside the vocabulary, or an excluded one (logit -inf),
+ * has -inf; a row of nothing else -inf everywhere and entropy 0; a row with a NaN or +inf, or an index outside [0, rows), NaN and alternatives
+ * -1.  Sums of 8192 tokens are in 32 bits, all others in 64; a row's results do not depend on what else is asked.  Scratch lies in the workspace:
+ * calls that share it are ordered by the caller. */
 enum { HS_LOGPROBS_TOP = 32 };
 typedef struct hs_logprobs_args {
     const void* logits;         /* DEVICE [rows][logits_stride]; with emitted also NULL: those of the step (hs_step.logits or the workspace's) */

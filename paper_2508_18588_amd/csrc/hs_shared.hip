@@ -358,10 +358,19 @@ __global__ __launch_bounds__(256) void shared_merge(shr_args a) {
 // 125 us, in partitions of 512 to 2048 keys by one to four workgroups 117 to 161; 256 sequences with drafts, 2048 own tokens, 163, 168 to 200; 7
 // sequences of up to 1900 tokens, 2 KV heads, 52 and 16.  With fewer sequences a workgroup per partition, as many as four for every compute unit.
 //
-// A prefix is cut into as many runs as make two workgroups for every compute unit, three at least, so that the last ones to start are short: 64 trees
+// A prefix is cut into as many runs as two workgroups for every compute unit take, three at least, so that the last ones to start are short: 64 trees
 // of 17 nodes behind 8000 tokens, 8 KV heads, with 1, 2, 3, 4 and 6 runs 232, 244, 209, 224 and 232 us, the drafts 232, 176, 163, 164 and 164, single tokens
-// 144, 121, 125, 127 and 129 (more runs keep the long walks of own keys waiting), 7 sequences behind 700 tokens 24, 19, 17, 16 and 16.
-constexpr int SHARED_WHOLE_KEYS = 16000, SHARED_SHORT_KEYS = 160, SHARED_RUNS = 3, SHARED_RUN_TILES = 4;
+// 144, 121, 125, 127 and 129 (more runs keep the long walks of own keys waiting), 7 sequences behind 700 tokens 24, 19, 17, 16 and 16; 16 trees behind 4096
+// tokens with as many runs as fit at once, five, 52, with six 59.  Where the rows alone fill the chip a run has sixteen tiles at least, since a partial
+// result costs what it takes to write and read: 128 trees of 8 prompts behind 512 tokens with one run 67, with three 85; the drafts behind 512 with one 51, with
+// three 48, behind 2048 as many as before.
+//
+// With short tables nothing is shared: the prefix lies in the caches, each sequence walks it with its own keys, and there are no partial results and no
+// second launch.  7 sequences of 64 + 32 tokens 8.3 us, with sharing 10.7, 128 + 64: 10.1 and 11.5, 256 + 64: 13.0 and 11.5; with many sequences
+// the walks overlap: 128 single tokens 256 + 64 15.3 and 17.1, the drafts 300 + 70 44 and 43, 64 trees 300 + 70 22 and 39.  (Trees whose rows fill their tiles
+// would be faster alone up to 2000 tokens, 1024 + 64: 41 and 54; the drafts, within the same limits, slower, 80 and 57.)
+constexpr int SHARED_WHOLE_KEYS = 16000, SHARED_SHORT_KEYS = 160, SHARED_ALONE_MANY = 400, SHARED_ALONE_FEW = 208;
+constexpr int SHARED_RUNS = 3, SHARED_RUN_TILES = 4, SHARED_RUN_TILES_MANY = 16;
 struct shr_plan { int part_keys, max_parts, splits; bool whole; };
 shr_plan plan_keys(const hs_ctx* ctx, const hs_shared_prefix* pre) {
     const hs_limits& l = ctx->lim;
@@ -370,14 +379,16 @@ shr_plan plan_keys(const hs_ctx* ctx, const hs_shared_prefix* pre) {
     const long long span = std::max<long long>(cap - longest, 32), pairs = (long long)l.max_batch * d.n_kv_heads;
     shr_plan p;
     p.whole = span <= (pairs >= ctx->n_cu ? SHARED_WHOLE_KEYS : SHARED_SHORT_KEYS);
+    const bool alone = cap <= (2 * pairs >= ctx->n_cu ? SHARED_ALONE_MANY : SHARED_ALONE_FEW);
+    p.whole |= alone;
     long long part = 2048;
     while (part > ctx->att_part && pairs * ((span + part - 1) / part) < 4ll * ctx->n_cu) part /= 2;
     p.part_keys = (int)std::max<long long>(part, ctx->att_part);      // (a table's keys in partitions of att_part: max_parts)
     p.max_parts = ctx->max_parts + hs_shared_runs(ctx);
     const long long rows = (long long)(d.n_q_heads / d.n_kv_heads) * pre->max_members * (1 + l.c_max * l.k_max), tiles = longest / 32;
     const long long units = (long long)pre->n_groups * d.n_kv_heads * ((rows + 127) / 128);
-    const long long want = std::max<long long>(SHARED_RUNS, (2 * ctx->n_cu + units - 1) / units);
-    p.splits = tiles == 0 ? 0 : (int)std::max(1ll, std::min({want, (long long)hs_shared_runs(ctx), tiles / SHARED_RUN_TILES}));
+    const long long want = std::max<long long>(SHARED_RUNS, 2 * ctx->n_cu / units), least = units >= ctx->n_cu ? SHARED_RUN_TILES_MANY : SHARED_RUN_TILES;
+    p.splits = tiles == 0 || alone ? 0 : (int)std::max(1ll, std::min({want, (long long)hs_shared_runs(ctx), tiles / least}));
     return p;
 }
 
@@ -450,6 +461,7 @@ void hs_launch_shared_attention(const hs_ctx* ctx, int layer, const hs_kv_cache*
 void hs_launch_shared_merge(const hs_ctx* ctx, const hs_kv_cache* cache, const hs_seq_state* seq, const hs_step* step, const hs_shared_prefix* pre,
                             void* out, hipStream_t st) {
     const shr_args a = make_args(ctx, 0, cache, seq, step, pre, nullptr, out);
+    if (a.whole && a.splits == 0) return;      // (all rows have their results)
     const int per = 4 * 512 / ctx->desc.head_dim, sets = (a.hq + per - 1) / per;      // heads of a workgroup, workgroups of a row
     const dim3 grid(hs_row_grid(ctx, 256, sets), sets);
     const bool early = ctx->lim.max_rows <= HS_EARLY_ROWS;

@@ -67,8 +67,8 @@ class Engine:
         without workspace_logits, which keeps them inside the library's workspace) no logits array exists and the
         argmax comes out of the LM head's epilogue.  precise: run in the library's fp32-activation mode (plain
         kernels, float KV cache).  pages: the cache is a pool of so many pages, none of which a sequence holds yet (reserve(), fork(),
-        free_pages(), compact(); load_sequences() leaves them as they are); without it every sequence has pages for its maximum length from the
-        start."""
+        free_pages(), compact(); load_sequences() leaves them as they are, so pages that sequences share are freed before other texts are
+        loaded); without it every sequence has pages for its maximum length from the start."""
         self.shape = shape
         self.dev = torch.device("cuda:0")
         L = len(weights["wqkv"]) if n_layers is None else n_layers

@@ -20,7 +20,7 @@ def model():
 def engine(model, **kw):
     from paper_2508_18588_amd.runtime import Engine
     shape, w, rope, prompts = model
-    return Engine(shape, w, rope, max_batch=GROUPS * MEMBERS, k_max=4, c_max=1, max_len=160, max_rows=128, **kw)
+    return Engine(shape, w, rope, max_batch=GROUPS * MEMBERS, k_max=4, c_max=1, max_len=420, max_rows=128, **kw)
 
 
 def i32(a):

@@ -19,8 +19,9 @@ def share(eng, off, pre):
     eng.set_shared_prefix(off, pre)
 
 
-def build(heads, off, pre, own, kinds, seed=0, spare=0, **kw):
-    """An engine of groups off[] with prefixes pre[], own tokens own[b] and rows kinds[b] (a number of nodes, or parents)."""
+def build(heads, off, pre, own, kinds, seed=0, spare=450, **kw):
+    """An engine of groups off[] with prefixes pre[], own tokens own[b] and rows kinds[b] (a number of nodes, or parents).  spare: room in the tables for
+    more tokens (with short tables every sequence reads the prefix for itself)."""
     hq, hkv, hd = heads
     group = np.full(len(own), -1)
     for g in range(len(pre)):
@@ -60,17 +61,19 @@ CASES = [
 ]
 
 
+@pytest.mark.parametrize("spare", [0, 450])
 @pytest.mark.parametrize("case", range(len(CASES)))
-def test_against_the_definition(case):
+def test_against_the_definition(case, spare):
     heads, off, pre, own, kinds = CASES[case]
-    eng, lens, pars, q = build(heads, off, pre, own, kinds, seed=case)
+    eng, lens, pars, q = build(heads, off, pre, own, kinds, seed=case, spare=spare)
     check(attend(eng, q), eng, lens, pars, q, ALL, 0)
     eng.close()
 
 
+@pytest.mark.parametrize("spare", [0, 450])
 @pytest.mark.parametrize("pre", [1, 15, 16, 17, 32, 33, 47, 48, 63, 64, 65, 255, 256, 257, 1023, 1025])
-def test_prefixes_of_every_rest(pre):
-    eng, lens, pars, q = build((8, 2, 64), [0, 5], [pre], [1, 2, 16, 17, 40], [1, 3, -5, 1, 2], seed=pre)
+def test_prefixes_of_every_rest(pre, spare):
+    eng, lens, pars, q = build((8, 2, 64), [0, 5], [pre], [1, 2, 16, 17, 40], [1, 3, -5, 1, 2], seed=pre, spare=spare)
     check(attend(eng, q), eng, lens, pars, q, ALL, 0)
     eng.close()
 
@@ -95,7 +98,7 @@ def test_many_sequences_and_long_texts(hd):
 def test_short_tables():
     """Tables of few pages: no room for a second partial result."""
     for cap in (1, 17, 60, 100, 130, 200):
-        eng, lens, pars, q = build((4, 2, 64), [0, 3], [min(cap, 96)], [1 + cap // 3, 1, 2], [1, 1, 1], seed=cap)
+        eng, lens, pars, q = build((4, 2, 64), [0, 3], [min(cap, 96)], [1 + cap // 3, 1, 2], [1, 1, 1], seed=cap, spare=0)
         check(attend(eng, q), eng, lens, pars, q, ALL, 0)
         eng.close()
 
@@ -155,10 +158,11 @@ def test_nothing_to_see():
     eng.close()
 
 
+@pytest.mark.parametrize("spare", [40, 450])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-def test_unseen_places_have_no_influence(bad):
+def test_unseen_places_have_no_influence(bad, spare):
     """Slots behind the last node, draft nodes that are no ancestors, and other sequences' pages hold infinities or NaNs."""
-    eng, lens, pars, q = build((8, 2, 128), [0, 3], [100], [9, 30, 44], [-6, 1, -9], seed=8, spare=40)
+    eng, lens, pars, q = build((8, 2, 128), [0, 3], [100], [9, 30, 44], [-6, 1, -9], seed=8, spare=spare)
     hkv, hd = 2, 128
     kc = eng.kc.view(torch.bfloat16).view(eng.n_blocks, hkv, 16, hd)
     vc = eng.vc.view(torch.bfloat16).view(eng.n_blocks, hkv, hd, 16)
