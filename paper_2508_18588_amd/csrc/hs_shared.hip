@@ -12,7 +12,7 @@
 // With 16 responses of one token, 28 query and 4 KV heads, a key is multiplied with 112 query rows per KV head: prefixes are bound by the matrix unit
 // and own keys by memory, and both kinds of workgroups are in one launch, so that the ones' products and the others' loads overlap.  Times here
 // are those of both launches.  16 prompts of 1500 to 4500 tokens, 16 sequences each with drafts and up to 2048 own tokens, 4 KV heads: prefixes alone
-// 108 us, own keys alone 115 (4.2 TB/s), together 163; 64 trees of 17 nodes behind 8000 tokens, 40 and 8 heads: 209 us, 200 of them the prefix
+// 108 us, own keys alone 115 (4.2 TB/s), together 161; 64 trees of 17 nodes behind 8000 tokens, 40 and 8 heads: 204 us, nearly all of them the prefix
 // (880 TFLOP/s; the matrix unit is busy 47 % of the time, the vector unit 53 %, LDS 24 %, two wavefronts per SIMD to overlap them).
 //
 // The order of a row's sums is that of its keys: 32-key tiles; the runs of a prefix, which depend on its length, the limits and the hints given with
