@@ -103,11 +103,12 @@ def test_short_tables():
         eng.close()
 
 
+@pytest.mark.parametrize("spare", [0, 450])
 @pytest.mark.parametrize("gone", [[0], [0, 1], [2], [0, 3], [0, 1, 2, 3]])
-def test_members_without_rows(gone):
+def test_members_without_rows(gone, spare):
     """The first member that has rows is whose table is read: the others' entries may be gone."""
     kinds = [None if b in gone else [1, 3, -4, 2][b % 4] for b in range(6)]
-    eng, lens, pars, q = build((4, 2, 128), [0, 4, 6], [300, 50], [20, 30, 40, 50, 60, 70], kinds, seed=9)
+    eng, lens, pars, q = build((4, 2, 128), [0, 4, 6], [300, 50], [20, 30, 40, 50, 60, 70], kinds, seed=9, spare=spare)
     for b in gone:
         eng.block_table[b] = -1
         eng.seq_len[b] = 0
@@ -115,9 +116,10 @@ def test_members_without_rows(gone):
     eng.close()
 
 
-def test_prefix_beyond_what_a_member_has_cached():
+@pytest.mark.parametrize("spare", [0, 450])
+def test_prefix_beyond_what_a_member_has_cached(spare):
     """It is cut to what all members with rows have cached: a prefix length that runs ahead does not change what a row sees."""
-    eng, lens, pars, q = build((8, 2, 64), [0, 4], [320], [10, 20, 30, 40], [1, 2, -3, 1], seed=4)
+    eng, lens, pars, q = build((8, 2, 64), [0, 4], [320], [10, 20, 30, 40], [1, 2, -3, 1], seed=4, spare=spare)
     eng.set_shared_prefix([0, 4], [2 ** 31 - 1])
     for b in range(4):      # (all tables name the same pages for all positions that may be shared then)
         eng.block_table[b, :(min(lens) - 1) // 16] = eng.block_table[0, :(min(lens) - 1) // 16]
@@ -125,8 +127,9 @@ def test_prefix_beyond_what_a_member_has_cached():
     eng.close()
 
 
-def test_missing_pages_are_not_seen():
-    eng, lens, pars, q = build((8, 2, 128), [0, 3, 4], [400, 64], [100, 200, 30, 90], [1, 9, -5, 2], seed=5)
+@pytest.mark.parametrize("spare", [0, 450])
+def test_missing_pages_are_not_seen(spare):
+    eng, lens, pars, q = build((8, 2, 128), [0, 3, 4], [400, 64], [100, 200, 30, 90], [1, 9, -5, 2], seed=5, spare=spare)
     holes = {0: [2, 3, 9], 1: [2, 3, 9, 30], 2: [2, 3, 9], 3: [0, 5]}
     for b, pages in holes.items():
         for i, p in enumerate(pages):
@@ -147,9 +150,10 @@ def test_missing_pages_are_not_seen():
     eng.close()
 
 
-def test_nothing_to_see():
+@pytest.mark.parametrize("spare", [0, 450])
+def test_nothing_to_see(spare):
     """Rows whose pages are all missing, sequences of no tokens: zeros."""
-    eng, lens, pars, q = build((4, 2, 64), [0, 3], [64], [5, 6, 7], [1, 2, 1], seed=6)
+    eng, lens, pars, q = build((4, 2, 64), [0, 3], [64], [5, 6, 7], [1, 2, 1], seed=6, spare=spare)
     eng.block_table[:] = -1
     out = attend(eng, q)
     assert (out == 0).all()
@@ -177,9 +181,10 @@ def test_unseen_places_have_no_influence(bad, spare):
     eng.close()
 
 
-def test_seen_nonfinite_values_are_the_rows_own():
+@pytest.mark.parametrize("spare", [0, 450])
+def test_seen_nonfinite_values_are_the_rows_own(spare):
     """A NaN in a prefix's values reaches every member's rows in that element, one in a sequence's own value its rows alone."""
-    eng, lens, pars, q = build((4, 2, 64), [0, 3], [96], [20, 30, 40], [1, 2, 1], seed=3)
+    eng, lens, pars, q = build((4, 2, 64), [0, 3], [96], [20, 30, 40], [1, 2, 1], seed=3, spare=spare)
     vc = eng.vc.view(torch.bfloat16).view(eng.n_blocks, 2, 64, 16)
     vc[int(eng.block_table[1, (lens[1] - 5) // 16]), 1, 7, (lens[1] - 5) % 16] = float("nan")
     out = attend(eng, q).float().view(-1, 4, 64)
@@ -224,8 +229,9 @@ def test_small_hints_still_compute_everything():
     eng.close()
 
 
-def test_rows_behind_the_last_and_in_place():
-    eng, lens, pars, q = build((4, 2, 64), [0, 3], [64], [5, 6, 7], [1, 2, 1], seed=13, max_rows=40)
+@pytest.mark.parametrize("spare", [0, 450])
+def test_rows_behind_the_last_and_in_place(spare):
+    eng, lens, pars, q = build((4, 2, 64), [0, 3], [64], [5, 6, 7], [1, 2, 1], seed=13, spare=spare, max_rows=40)
     want = attend(eng, q)
     big = torch.full((12, q.shape[1]), 3.0, device="cuda:0", dtype=torch.bfloat16)
     big[:4] = q
@@ -234,8 +240,9 @@ def test_rows_behind_the_last_and_in_place():
     eng.close()
 
 
-def test_other_layers_and_streams():
-    eng, lens, pars, q = build((4, 2, 64), [0, 3], [100], [5, 60, 7], [1, 2, -4], seed=14, layers=3)
+@pytest.mark.parametrize("spare", [0, 450])
+def test_other_layers_and_streams(spare):
+    eng, lens, pars, q = build((4, 2, 64), [0, 3], [100], [5, 60, 7], [1, 2, -4], seed=14, spare=spare, layers=3)
     for layer in range(3):
         check(attend(eng, q, layer), eng, lens, pars, q, ALL, 0, layer=layer)
     want, side = attend(eng, q, 1), torch.cuda.Stream()
@@ -256,9 +263,10 @@ def test_precise_mode_reads_every_table():
     eng.close()
 
 
-def test_captured_and_replayed():
+@pytest.mark.parametrize("spare", [0, 450])
+def test_captured_and_replayed(spare):
     """A graph keeps the arrays, not their contents: prefixes and lengths may change between replays."""
-    eng, lens, pars, q = build((8, 2, 64), [0, 3, 5], [200, 64], [50, 60, 70, 80, 90], [1, 2, 3, 1, 2], seed=16)
+    eng, lens, pars, q = build((8, 2, 64), [0, 3, 5], [200, 64], [50, 60, 70, 80, 90], [1, 2, 3, 1, 2], seed=16, spare=spare)
     out = torch.zeros_like(q)
     eng.attention_shared(0, q, out)
     torch.cuda.synchronize()
@@ -278,9 +286,10 @@ def test_captured_and_replayed():
     eng.close()
 
 
-def test_a_graph_of_other_groups():
+@pytest.mark.parametrize("spare", [0, 450])
+def test_a_graph_of_other_groups(spare):
     """Prefixes set anew leave the arrays that a recorded graph reads where they are; its groups that there are no more are empty."""
-    eng, lens, pars, q = build((8, 2, 64), [0, 2, 4, 5], [200, 64, 96], [50, 60, 70, 80, 90], [1, 2, 3, 1, 2], seed=18)
+    eng, lens, pars, q = build((8, 2, 64), [0, 2, 4, 5], [200, 64, 96], [50, 60, 70, 80, 90], [1, 2, 3, 1, 2], seed=18, spare=spare)
     out = torch.zeros_like(q)
     eng.attention_shared(0, q, out)
     torch.cuda.synchronize()
@@ -296,9 +305,10 @@ def test_a_graph_of_other_groups():
     eng.close()
 
 
-def test_text_beyond_the_table():
+@pytest.mark.parametrize("spare", [0, 450])
+def test_text_beyond_the_table(spare):
     """Of a sequence that has outgrown its table a row sees what the table holds, in a prefix and in its own keys."""
-    eng, lens, pars, q = build((8, 2, 64), [0, 3], [128], [30, 40, 50], [1, 1, 1], seed=19)
+    eng, lens, pars, q = build((8, 2, 64), [0, 3], [128], [30, 40, 50], [1, 1, 1], seed=19, spare=spare)
     cap = 16 * eng.max_blocks
     for ahead in (1, 17, 5000, 2 ** 31 - 2 - cap):
         eng.seq_len[1] = min(cap + ahead, 2 ** 31 - 1)
