@@ -7,8 +7,8 @@
 // A row's k largest tokens lie in units whose maximum is not below the k-th largest one (k units have a token as large): the second launch reads little
 // more than k units again.
 // Chunks and units belong to the vocabulary alone: a row's results have the same bits whatever else is asked.
-// 1088 rows of 152064 floats with 20 alternatives: 117 us for the first launch (5.7 TB/s, of the 6.2 that reads alone reach) and 22 for the second;
-// the emitted tokens of 64 sequences, without alternatives, 20 and 3.5; 7 rows of bf16 with 5: 4.6 and 7.5, two chains of round trips to memory.
+// 1088 rows of 152064 floats with 20 alternatives: 117 us for the first launch (5.7 TB/s, of the 6.2 that reads alone reach) and 14 for the second;
+// the emitted tokens of 64 sequences, without alternatives, 20 and 3.5; 7 rows of bf16 with 5: 4.6 and 8, two chains of round trips to memory.
 #include <algorithm>
 #include <cmath>
 
@@ -245,6 +245,7 @@ __device__ __forceinline__ void pick_tokens(const T* __restrict__ row, int vocab
         }
     __syncthreads();
     const int n_units = l.n_units;
+    const bool aligned = ((unsigned long long)row & 15ull) == 0;
     auto token = [&](int q) { return l.unit[q] * UNIT + tid; };
     auto logit = [&](int q) { return token(q) < vocab ? wide(row[token(q)]) : -INFINITY; };
     bool fits = n_units <= LEFT;
@@ -257,17 +258,35 @@ __device__ __forceinline__ void pick_tokens(const T* __restrict__ row, int vocab
             bound = max(bound, lower_bound(most, k, l, [] {}));
         }
         if (turn == 0 && bound == 0 && n_units > 1) continue;      // (no bound: that of the tokens at once)
-        // (sixteen on their way: the units are no longer in the caches, and a trip to memory takes longer than the rest)
-        for (int q0 = 0; q0 < n_units; q0 += 16) {
-            float v[16];
+        // Thirty-two units on their way, a wavefront has whole ones in runs of 16 bytes: they are no longer in the caches, and a trip to memory takes longer
+        // than the rest.  (A token per thread and sixteen units on their way: 1088 rows of 152064 floats, 20 alternatives, 141 us, so 136; 128 rows 39 and 34;
+        // 7 rows 16 and 14; 1088 rows of 32000 bf16 logits 41 and 33.)
+        constexpr int RUN = run_of<T>, PER = 64 * RUN / UNIT, LOADS = 8 / PER;
+        for (int q0 = 0; q0 < n_units; q0 += 32) {
+            float v[LOADS][RUN];
+            const bool second = q0 + 16 < n_units;      // (with few alternatives there are no more than sixteen)
+            auto first = [&](int r) {
+                const int q = q0 + (r * 4 + (tid >> 6)) * PER + lane * PER / 64;
+                return q < n_units ? l.unit[q] * UNIT + lane * RUN % UNIT : vocab;
+            };
+            auto load = [&](int r0) {
 #pragma unroll
-            for (int q = 0; q < 16; q++) v[q] = q0 + q < n_units ? logit(q0 + q) : -INFINITY;
+                for (int r = r0; r < r0 + LOADS / 2; r++) load_run<T>(row, first(r), vocab, aligned, v[r]);
+            };
+            auto take = [&](int r0) {
 #pragma unroll
-            for (int q = 0; q < 16; q++)
-                if (in_running(v[q], bound)) {
-                    const int at = atomicAdd(&l.n_tokens, 1);
-                    if (at < LEFT) l.token[at] = key_of(v[q], token(q0 + q));
-                }
+                for (int r = r0; r < r0 + LOADS / 2; r++)
+#pragma unroll
+                    for (int e = 0; e < RUN; e++)
+                        if (in_running(v[r][e], bound)) {
+                            const int at = atomicAdd(&l.n_tokens, 1);
+                            if (at < LEFT) l.token[at] = key_of(v[r][e], first(r) + e);
+                        }
+            };
+            load(0);
+            if (second) load(LOADS / 2);
+            take(0);
+            if (second) take(LOADS / 2);
         }
         __syncthreads();
         if (l.n_tokens <= LEFT) break;
