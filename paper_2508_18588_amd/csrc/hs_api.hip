@@ -33,13 +33,15 @@ void layout_workspace(hs_ctx* ctx) {
     w.err = take(256);
     w.x = take(M * d.d_model * 4);
     w.xn = take(M * d.d_model * ab);
-    w.qkv = take(M * nqkv * 4);
+    // The attention's partial results.  Those of a shared prefix's runs follow a sequence's own partitions, over arrays that hold nothing while
+    // attention runs: the projected QKV rows, which are queries and cache by then, and below the projections' partial sums, which have been
+    // added up.  (Room of their own was 346 MB for 16384 rows of 28 heads, in every context.)
+    const size_t heads = M * d.n_q_heads, runs = (size_t)hs_shared_runs(ctx);
+    w.part_ml = take(heads * ctx->max_parts * 2 * 4);
+    w.qkv = take(std::max(M * nqkv * 4, heads * runs * 2 * 4));
     w.q = take(M * qh * ab);
     w.attn = take(M * qh * ab);
     w.act = take(M * (size_t)d.d_ffn * ab);
-    const size_t parts = (size_t)(ctx->max_parts + hs_shared_runs(ctx));   // (a shared prefix's runs behind a sequence's own partitions)
-    w.part_o = take(M * d.n_q_heads * parts * d.head_dim * 2);   // fp16
-    w.part_ml = take(M * d.n_q_heads * parts * 2 * 4);
     w.logits_bytes = hs_logits_in_workspace(ctx) ? M * (size_t)d.vocab * 4 : 0;
     w.logits = take(w.logits_bytes);
     w.rowmax = take(M * (size_t)hs_gemm_rowmax_groups(d.vocab) * 8);
@@ -52,7 +54,10 @@ void layout_workspace(hs_ctx* ctx) {
                                  (size_t)std::max(hs_gemm_chunks(d.d_model, d.d_ffn), hs_gemm_chunks(d.d_model, d.d_ffn, false)) * d.d_model,
                                  lm_chunks > 1 ? (size_t)lm_chunks * d.vocab : (size_t)0});
     w.gemm_part_bytes = M * part_cols * 4;
-    w.gemm_part = take(w.gemm_part_bytes);
+    // (the log probabilities' scratch, too: neither attention nor projections run meanwhile, calls that share the workspace are ordered)
+    w.logprobs = w.part_o = take(heads * ctx->max_parts * d.head_dim * 2);   // fp16
+    w.gemm_part = take(std::max(w.gemm_part_bytes, heads * runs * d.head_dim * 2));
+    take(w.logprobs + hs_logprobs_scratch(d.vocab) > off ? w.logprobs + hs_logprobs_scratch(d.vocab) - off : 0);
     w.pf_len = take((size_t)l.max_batch * 4);
     w.row_info = take(M * sizeof(hs_row_info));
     w.att_work = take((size_t)(2 + d.n_layers) * 4);
@@ -62,7 +67,6 @@ void layout_workspace(hs_ctx* ctx) {
     w.probs_sums = take((size_t)HS_PROBS_ROUNDS * l.max_batch * hs_probs_slices(d.vocab) * sizeof(double));
     w.probs_records = take((size_t)HS_PROBS_ROUNDS * l.max_batch * HS_PROBS_RECORD);
     w.probs_stats = take(HS_PROBS_STATS * 8);
-    w.logprobs = take(hs_logprobs_scratch(d.vocab));
     w.shared_parts = take((size_t)l.max_batch * 4);
     w.total = off;
 }
