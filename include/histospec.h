@@ -448,7 +448,7 @@ typedef struct hs_logprobs_args {
     int64_t logits_stride;      /* elements, >= vocab (this and the next two are not read if logits is NULL) */
     int32_t logits_type;        /* HS_F32 or HS_BF16 */
     int32_t rows;
-    int32_t n;                  /* HOST: entries (not read with emitted) */
+    int32_t n;                  /* HOST: entries (not read with emitted); 0: nothing is asked, and arrays may be NULL */
     int32_t emitted;
     float temperature;          /* 1e-30 to 1e30 */
     int32_t top;                /* 0..HS_LOGPROBS_TOP, at most the vocabulary */

@@ -707,12 +707,14 @@ hs_status hs_attention_shared(hs_ctx* ctx, const hs_kv_cache* cache, const hs_se
 hs_status hs_logprobs(hs_ctx* ctx, const hs_logprobs_args* args, const hs_seq_state* seq, const hs_step* step, hs_stream stream) {
     if (!ctx) return HS_ERR_INVALID_ARG;
     if (!ctx->ws) return fail(ctx, HS_ERR_CAPACITY, "no workspace bound");
-    if (!args || !args->logprob) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: null output");
+    if (!args) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: arguments");
+    const bool nothing = !args->emitted && args->n == 0;      // (arrays of nothing may be anywhere, or nowhere)
+    if (!nothing && !args->logprob) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: null output");
     if (!(args->temperature >= 1e-30f && args->temperature <= 1e30f))
         return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: temperature must be positive and finite (1e-30 to 1e30)");
     if (args->top < 0 || args->top > HS_LOGPROBS_TOP || args->top > ctx->desc.vocab)
         return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: top");
-    if (args->top > 0 && (!args->top_token || !args->top_logprob)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: null alternatives");
+    if (!nothing && args->top > 0 && (!args->top_token || !args->top_logprob)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: null alternatives");
     const void* logits = args->logits;
     long long stride = args->logits_stride;
     int type = args->logits_type, rows = args->rows;
@@ -729,14 +731,14 @@ hs_status hs_logprobs(hs_ctx* ctx, const hs_logprobs_args* args, const hs_seq_st
             rows = ctx->lim.max_rows;
         }
     } else {
-        if (!logits) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: null logits");
+        if (!nothing && !logits) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: null logits");
         if (args->n < 0) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: n");
         if (args->n > 0 && !args->token) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: null tokens");
     }
     if (!type_ok(type)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: type");
     if (rows < 0) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: rows");
     if (!rows_ok(ctx, logits, stride, type)) return fail(ctx, HS_ERR_INVALID_ARG, "hs_logprobs: stride below the vocabulary, or misaligned rows");
-    if (!args->emitted && args->n == 0) return HS_OK;
+    if (nothing) return HS_OK;
     (void)hipGetLastError();
     hs_launch_logprobs(ctx, args, seq, step, logits, stride, type, rows, (hipStream_t)stream);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail_hip(ctx, "hs_logprobs", e);
