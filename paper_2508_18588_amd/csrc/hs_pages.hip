@@ -250,9 +250,9 @@ __global__ __launch_bounds__(256) void pages_fork(page_args a) {
     int32_t* row = a.table + (size_t)b * a.max_blocks;
     const int32_t* of = a.table + (size_t)p * a.max_blocks;
     for (int i = tid; i < a.max_blocks; i += 256) {
-        const int old = row[i], now = i < full ? of[i] : i == full ? own : -1;
+        const int old = row[i], page = i < full ? of[i] : i == full ? own : -1, now = is_page(a, page) ? page : -1;
         if (now == old) continue;
-        if (is_page(a, now)) atomicAdd(a.refs + now, 1);
+        if (now >= 0) atomicAdd(a.refs + now, 1);
         if (is_page(a, old)) drop_page(a, old);
         row[i] = now;
     }
