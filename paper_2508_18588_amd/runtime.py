@@ -192,9 +192,13 @@ class Engine:
     # ---------------------------------------------------------------- state loading (inputs only)
 
     def load_sequences(self, token_lists, budgets, seq_ids=None, k_init: int = 2):
-        """Set the committed tokens of each sequence (no K/V is computed here)."""
+        """Set the committed tokens of each sequence (no K/V is computed here).  No sequences share a prefix from here on, in recorded graphs
+        either, until set_shared_prefix() says so of the new texts."""
         B = len(token_lists)
         assert 1 <= B <= self.max_batch
+        if self._shared_arrays is not None:
+            self._shared_arrays[1].zero_()
+            self.set_shared_prefix(None)
         self.batch = B
         tok = np.zeros((self.max_batch, self.tokens_stride), np.int32)
         tail = np.zeros((self.max_batch, self.w_max), np.int32)
@@ -385,7 +389,9 @@ class Engine:
 
     def set_shared_prefix(self, group_off, prefix_len=None):
         """verify() and attention_shared() read the first prefix_len[g] positions of sequences group_off[g] .. group_off[g + 1] - 1, which hold the
-        same pages there, once for all of them; group_off = None: no sequences share."""
+        same pages there, once for all of them; group_off = None: no sequences share (a recorded graph goes on with what was set last).  It
+        holds until load_sequences().  Nothing checks that the pages are the same: after a fork() from another prompt, and after free_pages() of
+        a prefix that some members go on with, say it anew before the next step."""
         if group_off is None:
             self.shared = None
             hs_set_shared_prefix(self.ctx, None)
