@@ -316,8 +316,10 @@ typedef struct hs_shared_prefix {
 
 /* hs_verify reads shared prefixes once per group instead of once per sequence from the next call on, in layers without a window (with the
  * plain-kernel flags and in layers with one every sequence reads its own table).  NULL: no sequences share.  The struct is copied; what a HIP
- * graph has recorded keeps it (the arrays' contents may change between replays).  Results are those without sharing but for the order of sums: a
- * row's does not depend on what other rows there are, but it does on prefix_len and the hints. */
+ * graph has recorded keeps it (the arrays' contents may change between replays).  Results are those without sharing but for the order of sums, which
+ * depends on prefix_len and the hints.  It does not depend on what other rows there are as long as every member that may have rows has cached its
+ * group's whole prefix, prefix_len <= seq_len - 1 (for a prompt of n tokens: 16 * ((n - 1) / 16), the pages that a fork shares); a longer prefix
+ * is cut to what the members with rows have, and a row's last bits then follow from who these are. */
 hs_status hs_set_shared_prefix(hs_ctx* ctx, const hs_shared_prefix* prefix);
 
 /* Attention of one layer for queries that the caller has, with shared prefixes read once: what hs_verify runs when they are set.  row_off,

@@ -16,7 +16,8 @@
 // (880 TFLOP/s; the matrix unit is busy 47 % of the time, the vector unit 53 %, LDS 24 %, two wavefronts per SIMD to overlap them).
 //
 // The order of a row's sums is that of its keys: 32-key tiles; the runs of a prefix, which depend on its length, the limits and the hints given with
-// the prefixes; own keys in partitions at multiples of part_keys.  It does not depend on what other rows there are.
+// the prefixes; own keys in partitions at multiples of part_keys.  It does not depend on what other rows there are, but through P where a member has not
+// cached the group's whole prefix.
 #include <algorithm>
 
 #include "hs_attention_ring.h"

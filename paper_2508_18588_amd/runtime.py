@@ -391,7 +391,8 @@ class Engine:
         """verify() and attention_shared() read the first prefix_len[g] positions of sequences group_off[g] .. group_off[g + 1] - 1, which hold the
         same pages there, once for all of them; group_off = None: no sequences share (a recorded graph goes on with what was set last).  It
         holds until load_sequences().  Nothing checks that the pages are the same: after a fork() from another prompt, and after free_pages() of
-        a prefix that some members go on with, say it anew before the next step."""
+        a prefix that some members go on with, say it anew before the next step.  With prefixes that all members have cached whole (of a prompt
+        of n tokens (n - 1) // 16 * 16, the pages that a fork shares) a sequence's results do not depend on who else has rows."""
         if group_off is None:
             self.shared = None
             hs_set_shared_prefix(self.ctx, None)
