@@ -354,23 +354,33 @@ __global__ __launch_bounds__(256) void shared_merge(shr_args a) {
 // How keys are cut and shared out: a function of the limits and of the hints that come with the prefixes (not of a step's rows), since the order of
 // a row's sums follows from it; and, from what rows to expect, how many workgroups a launch has.
 //
-// Own keys are one walk per (sequence, KV head) where there are as many of these as compute units and no more keys than SHARED_WHOLE_KEYS behind the
-// longest prefix, or so few keys that the walk is as short as a second partial result's way: 128 sequences of up to 4096 own tokens, 4 KV heads,
-// 125 us, in partitions of 512 to 2048 keys by one to four workgroups 117 to 161; 256 sequences with drafts, 2048 own tokens, 163, 168 to 200; 7
-// sequences of up to 1900 tokens, 2 KV heads, 52 and 16.  With fewer sequences a workgroup per partition, as many as four for every compute unit.
+// Own keys are one walk per (sequence, KV head) where the limits allow as many of these as compute units and at most SHARED_WHOLE_KEYS keys behind the
+// longest prefix, or so few keys that the walk is as short as a second partial result's way; else they are cut into partitions, a workgroup each as
+// far as there are no more than sixteen for every compute unit.  7 sequences of up to 1900 tokens, 2 KV heads: a walk 52 us, partitions 16.  More
+// sequences with 50 own tokens and more behind 1500 to 2048, 28 and 4 heads; both launches with whole walks and with partitions of 2048 keys, us:
+//
+//   own tokens to                      1500       2500       3500       5000       7000      10000      14000
+//   128 single tokens               54   67    83   96   108  114   147  141   198  173   273  223   376  305
+//   128 with drafts                 73   89    93  112   119  135   164  169   223  217   314  297   431  380
+//   64 trees, 40 and 8 heads       107  117   131  136   149  162   186  192   243  247   332  319   451  419
+//   10 of 128 places still taken    44   44    65   59    87   63   119   65   162   69   227   73   313   82
+//
+// (The limits do not tell how many places are taken.  At the end of a rollout a few long sequences walk their keys on a few compute units: up to 6000
+// keys that is up to twice as long as it could be, beyond it partitions are about as fast with all places taken.)
 //
 // A prefix is cut into as many runs as two workgroups for every compute unit take, three at least, so that the last ones to start are short: 64 trees
 // of 17 nodes behind 8000 tokens, 8 KV heads, with 1, 2, 3, 4 and 6 runs 232, 244, 209, 224 and 232 us, the drafts 232, 176, 163, 164 and 164, single tokens
 // 144, 121, 125, 127 and 129 (more runs keep the long walks of own keys waiting), 7 sequences behind 700 tokens 24, 19, 17, 16 and 16; 16 trees behind 4096
 // tokens with as many runs as fit at once, five, 52, with six 59.  Where the rows alone fill the chip a run has sixteen tiles at least, since a partial
 // result costs what it takes to write and read: 128 trees of 8 prompts behind 512 tokens with one run 67, with three 85; the drafts behind 512 with one 51, with
-// three 48, behind 2048 as many as before.
+// three 48, behind 2048 as many as before.  All of this is counted by the limits and the longest prefix: decoding without drafts under limits for drafts gets
+// fewer runs than it has room for, and a group with a shorter prefix as many runs as the longest, of a tile at least.
 //
 // With short tables nothing is shared: the prefix lies in the caches, each sequence walks it with its own keys, and there are no partial results and no
 // second launch.  7 sequences of 64 + 32 tokens 8.3 us, with sharing 10.7, 128 + 64: 10.1 and 11.5, 256 + 64: 13.0 and 11.5; with many sequences
 // the walks overlap: 128 single tokens 256 + 64 15.3 and 17.1, the drafts 300 + 70 44 and 43, 64 trees 300 + 70 22 and 39.  (Trees whose rows fill their tiles
 // would be faster alone up to 2000 tokens, 1024 + 64: 41 and 54; the drafts, within the same limits, slower, 80 and 57.)
-constexpr int SHARED_WHOLE_KEYS = 16000, SHARED_SHORT_KEYS = 160, SHARED_ALONE_MANY = 400, SHARED_ALONE_FEW = 208;
+constexpr int SHARED_WHOLE_KEYS = 6000, SHARED_SHORT_KEYS = 160, SHARED_ALONE_MANY = 400, SHARED_ALONE_FEW = 208;
 constexpr int SHARED_RUNS = 3, SHARED_RUN_TILES = 4, SHARED_RUN_TILES_MANY = 16;
 struct shr_plan { int part_keys, max_parts, splits; bool whole; };
 shr_plan plan_keys(const hs_ctx* ctx, const hs_shared_prefix* pre) {
@@ -436,7 +446,7 @@ shr_args make_args(const hs_ctx* ctx, int layer, const hs_kv_cache* cache, const
     a.runs = 1;
     if (!a.whole) {
         const long long cap = (long long)a.max_blocks * 16, own = (cap + a.part_keys - 1) / a.part_keys, pairs = (long long)a.batch * a.hkv;
-        a.runs = (int)std::max(1ll, std::min(own, (8ll * ctx->n_cu + pairs - 1) / pairs));
+        a.runs = (int)std::max(1ll, std::min(own, (16ll * ctx->n_cu + pairs - 1) / pairs));
     }
     a.own_units = a.batch * a.hkv * a.runs * a.tiles;
     a.prefix_units = (a.n_groups * a.hkv * a.splits + 7) / 8 * 8 * a.prefix_tiles;

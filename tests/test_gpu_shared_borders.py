@@ -99,3 +99,20 @@ def test_new_texts_share_nothing(model, recorded):  # noqa: F811
         eng.attention_shared(0, torch.zeros(m, shape.n_q_heads * shape.head_dim, device="cuda:0", dtype=torch.bfloat16),
                              torch.zeros(m, shape.n_q_heads * shape.head_dim, device="cuda:0", dtype=torch.bfloat16))
     eng.close()
+
+
+@pytest.mark.parametrize("own", [5900, 6000, 6100, 9000])
+def test_few_long_texts_in_a_large_batch(own):
+    """128 places of which four are taken: own keys in one walk or in partitions, as the table's length says; a row's bits are the same with all taken."""
+    rng = np.random.default_rng(own)
+    group = [own, 3000, 17, own // 2]
+    lens_own = group + [int(x) for x in rng.integers(1, 40, 124)]
+    kinds = [1, 3, -4, 2] + [1] * 124
+    eng, lens, pars, q = build((4, 2, 64), [0, 4, 128], [300, 96], lens_own, kinds, seed=own, spare=0)
+    full = attend(eng, q)
+    check(full, eng, lens, pars, q, ALL, 0)
+    few = pars[:4] + [None] * 124
+    m = lay_out(eng, lens, few)
+    out = attend(eng, q[:m].contiguous())
+    assert torch.equal(out, full[:m])
+    eng.close()
