@@ -8,7 +8,9 @@
 // more than k units again.
 // Chunks and units belong to the vocabulary alone: a row's results have the same bits whatever else is asked.
 // 1088 rows of 152064 floats with 20 alternatives: 117 us for the first launch (5.7 TB/s, of the 6.2 that reads alone reach) and 14 for the second;
-// the emitted tokens of 64 sequences, without alternatives, 20 and 3.5; 7 rows of bf16 with 5: 4.6 and 8, two chains of round trips to memory.
+// the emitted tokens of 64 sequences, without alternatives, 20 and 3.5; 7 rows of bf16 with 5: 4.6 and 8, two chains of round trips to memory.  Logits
+// of 16 bits, with as many instructions per logit, reach less of that rate: both launches with 20 alternatives, 1088 rows of 152064 90 us (3.7 TB/s), of 32000 33.
+// Rows that do not begin at 16 bytes are read element by element: 1088 rows of 50257 bf16 88 us and of 50256 42, in 32 bits 67 and 58.
 #include <algorithm>
 #include <cmath>
 
@@ -20,12 +22,12 @@ namespace {
 constexpr int CHUNK = 8192, UNIT = 256, CHUNK_UNITS = CHUNK / UNIT;
 constexpr int UNITS_LDS = 2048;      // a row's units in LDS; of larger vocabularies (from 524288 tokens on) they are read again from memory
 
-struct lp_stat { float m, s, e, unused; };      // largest logit; sums of w and w d, w = exp2(d), d = (l - m) log2(e) / T
+struct __attribute__((aligned(16))) lp_stat { float m, s, e; };      // largest logit; sums of w and w d, w = exp2(d), d = (l - m) log2(e) / T
 struct lp_args {
     const void* logits;
     size_t stride;
     int rows, vocab, n, first, top, chunks, units;      // first: the number of entry 0 of this launch
-    float c, inv_t;                                     // log2(e) / T
+    float c;                                            // log2(e) / T
     double t;
     const int32_t *row, *token, *live;
     // emitted tokens: entry (b, i) = the i-th one of sequence b
@@ -130,7 +132,7 @@ __global__ __launch_bounds__(256) void logprobs_stats(lp_args a) {
     __syncthreads();
     if (tid == 0)
         a.stats[(size_t)at * a.chunks + chunk] = {top, (s_sum[0][0] + s_sum[0][1]) + (s_sum[0][2] + s_sum[0][3]),
-                                                  (s_sum[1][0] + s_sum[1][1]) + (s_sum[1][2] + s_sum[1][3]), 0.f};
+                                                  (s_sum[1][0] + s_sum[1][1]) + (s_sum[1][2] + s_sum[1][3])};
 }
 
 // Keys in the order of what is looked for: larger values first, then lower numbers; no two are equal, and 0 is none.
@@ -347,7 +349,7 @@ __global__ __launch_bounds__(256, 8) void logprobs_join(lp_args a) {
     }
     // The chunks, by one wavefront, which has asked for the first ones (and for the token's logit) before it is its turn.  (What is picked from a row with
     // a NaN or +inf is not used.)
-    const lp_stat x0 = lane < a.chunks ? st[lane] : lp_stat{-INFINITY, 0.f, 0.f, 0.f};
+    const lp_stat x0 = lane < a.chunks ? st[lane] : lp_stat{-INFINITY, 0.f, 0.f};
     const float own = (unsigned)q.token < (unsigned)a.vocab ? wide(row[q.token]) : -INFINITY;
     auto join_chunks = [&]() {
         float m = x0.m;

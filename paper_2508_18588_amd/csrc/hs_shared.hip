@@ -12,7 +12,7 @@
 // With 16 responses of one token, 28 query and 4 KV heads, a key is multiplied with 112 query rows per KV head: prefixes are bound by the matrix unit
 // and own keys by memory, and both kinds of workgroups are in one launch, so that the ones' products and the others' loads overlap.  Times here
 // are those of both launches.  16 prompts of 1500 to 4500 tokens, 16 sequences each with drafts and up to 2048 own tokens, 4 KV heads: prefixes alone
-// 108 us, own keys alone 115 (4.2 TB/s), together 161; 64 trees of 17 nodes behind 8000 tokens, 40 and 8 heads: 204 us, nearly all of them the prefix
+// 108 us, own keys alone 114 (4.2 TB/s), together 160; 64 trees of 17 nodes behind 8000 tokens, 40 and 8 heads: 205 us, nearly all of them the prefix
 // (880 TFLOP/s; the matrix unit is busy 47 % of the time, the vector unit 53 %, LDS 24 %, two wavefronts per SIMD to overlap them).
 //
 // The order of a row's sums is that of its keys: 32-key tiles; the runs of a prefix, which depend on its length, the limits and the hints given with
@@ -368,7 +368,8 @@ __global__ __launch_bounds__(256) void shared_merge(shr_args a) {
 // (The limits do not tell how many places are taken.  At the end of a rollout a few long sequences walk their keys on a few compute units: up to 6000
 // keys that is up to twice as long as it could be, beyond it partitions are about as fast with all places taken.)
 //
-// A prefix is cut into as many runs as two workgroups for every compute unit take, three at least, so that the last ones to start are short: 64 trees
+// A prefix is cut into as many runs as two workgroups for every compute unit take, three at least, so that the last ones to start are short (all figures
+// of this paragraph by one build, in which the trees took 209 and the drafts 163, since then 205 and 160): 64 trees
 // of 17 nodes behind 8000 tokens, 8 KV heads, with 1, 2, 3, 4 and 6 runs 232, 244, 209, 224 and 232 us, the drafts 232, 176, 163, 164 and 164, single tokens
 // 144, 121, 125, 127 and 129 (more runs keep the long walks of own keys waiting), 7 sequences behind 700 tokens 24, 19, 17, 16 and 16; 16 trees behind 4096
 // tokens with as many runs as fit at once, five, 52, with six 59.  Where the rows alone fill the chip a run has sixteen tiles at least, since a partial

@@ -452,8 +452,8 @@ class Engine:
         hs_pages_free(self.ctx, self.c_cache, self.c_seq, self.c_pool, first.data_ptr(), end.data_ptr(), self.stream())
 
     def compact(self, moved=None):
-        """Moves the held pages to the lowest numbers; returns their number (int32 [1], on the device).  moved: int32 [n_blocks] for every page's new
-        number."""
+        """Moves the held pages to the lowest numbers; returns their number (int32 [1], on the device: the engine's own tensor, which the next call
+        overwrites).  moved: int32 [n_blocks] for every page's new number."""
         self._pooled()
         if moved is not None:
             if moved.dtype != torch.int32 or not moved.is_contiguous() or moved.numel() < self.n_blocks:
