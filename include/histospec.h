@@ -442,8 +442,8 @@ hs_status hs_probs(hs_ctx* ctx, const hs_probs_args* args, hs_stream stream);
  * sequence b has emitted in this step, i < n_out[b], out_tok[b][i] at the row of node path_row[b][i]: between acceptance and the next draft.
  * Entries that are not there (i >= *live, i >= n_out[b]) are left as they are.  A token outside the vocabulary, or an excluded one (logit -inf),
  * has -inf; a row of nothing else -inf everywhere and entropy 0; a row with a NaN or +inf, or an index outside [0, rows), NaN and alternatives
- * -1.  Sums of 8192 tokens are in 32 bits, all others in 64; a row's results do not depend on what else is asked.  Scratch lies in the workspace:
- * calls that share it are ordered by the caller. */
+ * -1.  Sums of 8192 tokens are in 32 bits, all others in 64; a row's results do not depend on what else is asked.  Scratch lies in the workspace,
+ * apart from that of other calls: calls of hs_logprobs that share it are ordered by the caller, others may run beside them. */
 enum { HS_LOGPROBS_TOP = 32 };
 typedef struct hs_logprobs_args {
     const void* logits;         /* DEVICE [rows][logits_stride]; with emitted also NULL: those of the step (hs_step.logits or the workspace's) */

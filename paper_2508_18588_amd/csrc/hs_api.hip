@@ -54,10 +54,8 @@ void layout_workspace(hs_ctx* ctx) {
                                  (size_t)std::max(hs_gemm_chunks(d.d_model, d.d_ffn), hs_gemm_chunks(d.d_model, d.d_ffn, false)) * d.d_model,
                                  lm_chunks > 1 ? (size_t)lm_chunks * d.vocab : (size_t)0});
     w.gemm_part_bytes = M * part_cols * 4;
-    // (the log probabilities' scratch, too: neither attention nor projections run meanwhile, calls that share the workspace are ordered)
-    w.logprobs = w.part_o = take(heads * ctx->max_parts * d.head_dim * 2);   // fp16
+    w.part_o = take(heads * ctx->max_parts * d.head_dim * 2);   // fp16
     w.gemm_part = take(std::max(w.gemm_part_bytes, heads * runs * d.head_dim * 2));
-    take(w.logprobs + hs_logprobs_scratch(d.vocab) > off ? w.logprobs + hs_logprobs_scratch(d.vocab) - off : 0);
     w.pf_len = take((size_t)l.max_batch * 4);
     w.row_info = take(M * sizeof(hs_row_info));
     w.att_work = take((size_t)(2 + d.n_layers) * 4);
@@ -67,6 +65,7 @@ void layout_workspace(hs_ctx* ctx) {
     w.probs_sums = take((size_t)HS_PROBS_ROUNDS * l.max_batch * hs_probs_slices(d.vocab) * sizeof(double));
     w.probs_records = take((size_t)HS_PROBS_ROUNDS * l.max_batch * HS_PROBS_RECORD);
     w.probs_stats = take(HS_PROBS_STATS * 8);
+    w.logprobs = take(hs_logprobs_scratch(d.vocab));   // (of their own: they may run beside the next step)
     w.shared_parts = take((size_t)l.max_batch * 4);
     w.total = off;
 }

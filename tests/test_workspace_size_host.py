@@ -1,4 +1,4 @@
-"""What a context's workspace takes: shared prefixes and log probabilities borrow arrays that are idle while they run (no GPU)."""
+"""What a context's workspace takes: shared prefixes borrow arrays that are idle while attention runs (no GPU)."""
 import ctypes as C
 
 import pytest
@@ -28,9 +28,9 @@ def workspace(shape, batch, k_max, c_max, rows, blocks):
     ("14b", (128, 16, 1, 2176, 256), 614012928), ("14b", (64, 8, 2, 16384, 560), 5469514496), ("14b", (16, 4, 1, 16384, 256), 6680275712),
     ("toy", (64, 8, 2, 16384, 560), 360683264),
 ])
-def test_large_contexts_hold_no_memory_for_operators_that_they_do_not_use(lib, shape, limits, without):  # noqa: F811
-    """But for a number per sequence and what a few arrays more are rounded up by."""
-    assert workspace(shape, *limits) <= without + 4096
+def test_large_contexts_hold_no_memory_for_prefixes_that_they_do_not_share(lib, shape, limits, without):  # noqa: F811
+    """But for the log probabilities' 16 MB, a number per sequence and what a few arrays more are rounded up by."""
+    assert workspace(shape, *limits) <= without + (16 << 20) + 4096
 
 
 @pytest.mark.parametrize("shape", list(SHAPES))
