@@ -24,7 +24,7 @@ def workspace(shape, batch, k_max, c_max, rows, blocks):
 @pytest.mark.parametrize("shape,limits,without", [
     # limits: sequences, k_max, c_max, rows, pages per sequence; bytes that the same context needs for all other calls
     ("1.5b", (64, 8, 2, 16384, 560), 4747430656), ("1.5b", (16, 4, 1, 16384, 256), 3760810752),
-    ("7b", (128, 16, 1, 2176, 256), 630724608), ("7b", (64, 8, 2, 16384, 560), 5941373696), ("7b", (256, 8, 1, 16384, 2048), 7639449088),
+    ("7b", (128, 16, 1, 2304, 256), 667659264), ("7b", (64, 8, 2, 16384, 560), 5941373696), ("7b", (256, 8, 1, 16384, 2048), 7639449088),
     ("14b", (128, 16, 1, 2176, 256), 614012928), ("14b", (64, 8, 2, 16384, 560), 5469514496), ("14b", (16, 4, 1, 16384, 256), 6680275712),
     ("toy", (64, 8, 2, 16384, 560), 360683264),
 ])
